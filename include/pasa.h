@@ -17,6 +17,12 @@
  *   pasa_forward          statistics, scores, routing and piecewise attention in one call
  *   pasa_forward_buffers  the same with the intermediates in the caller's buffers
  *
+ * For generation in chunks, where the keys and values of everything produced so far are kept, there is a cache in 4 bits:
+ *
+ *   pasa_cache_write      quantises rows of K and V into the pages of their sequences
+ *   pasa_cache_read       reads rows back as bf16
+ *   pasa_cache_attn       dense attention (Eq.1) of new rows over the cached tokens
+ *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless marked "host".  The caller owns every buffer; the
  *     library never allocates, frees or synchronises.  All work is enqueued on `stream`
@@ -321,6 +327,66 @@ PASA_API int pasa_l1_distance(const void* a, const void* b, int64_t n, int32_t d
                               size_t ws_bytes, void* stream);
 PASA_API int pasa_budget_schedule(const double* l1, int32_t n_prompts, int32_t n_steps, double rho,
                                   double dense_fraction, double* rho_t);
+
+/*
+ * Key/value cache in 4 bits.
+ *
+ * A cache is a pool of pages; a page holds `page` consecutive tokens of one sequence, keys and values of all heads.  Which
+ * pages a sequence has is the caller's business: pages [B, max_pages] names, for tokens j * page .. of sequence b, a page of the pool.
+ * Every group of `group` channels of a token has a scale s and a minimum m (bf16), every channel a code c of 4 bits, and the
+ * cache stands for s c + m:
+ *   m = smallest value of the group;  s = bf16(binary32((largest - m) / 15)), 0 if that is below 2^-126;
+ *   c = (x - m) / s rounded to the nearest integer, ties to even, at most 15  (0 if s = 0).
+ * A group that holds an infinity or a NaN reads back as NaN.
+ * Bytes: the pool is [n_pages][H_kv] runs; a run is K codes [page][d/2], V codes [page][d/2], K parameters [page][d/group],
+ * V parameters [page][d/group]; a parameter is s, then m.  A 32-bit word of codes holds 8 channels, channel i of them in bits
+ * 4i .. 4i+3; word w of a token's V codes holds the channels 8w .. 8w+7, word q * (d/32) + j of its K codes the channels
+ * 32j + 8q .. 32j + 8q + 7 (q = 0 .. 3).
+ *
+ * Rows.  The three calls share one convention: len [B] counts the tokens of each sequence including the rows of this step, n_new [B] (NULL:
+ * shape->n for all) the rows of this step, and row i < n_new[b] of a [B, H, n, d] tensor is token len[b] - n_new[b] + i.  Rows at and
+ * behind n_new[b] are padding: neither read nor written.  n_new is taken as at most n and at least 0, len as at least 0, and no token
+ * beyond max_pages * page is looked at.  A step of a model is pasa_cache_write of its K and V, then pasa_cache_attn of its Q with the same
+ * len and n_new.
+ *   shape   B, H, n, d, strides and (pasa_cache_attn) scale of the row tensors; block, group and kv_slices are not looked at
+ *   pool    pool_bytes >= pasa_cache_bytes(cache) bytes, 16-byte aligned
+ *   pages   int32 [B, max_pages];  len, n_new  int32 [B]: all on the device, so that a captured graph can be replayed while
+ *           sequences grow.  A page number outside [0, n_pages) is not followed: its tokens are not written, not read (the rows keep
+ *           what they held) and seen by no query.  A page written for two sequences in one call holds either's bytes.
+ */
+typedef struct {
+  int32_t H_kv;      /* key/value heads                                                  */
+  int32_t d;         /* head dimension, 64 or 128                                        */
+  int32_t group;     /* channels that share a scale and a minimum: 32, 64 or 128, at most d */
+  int32_t page;      /* tokens of a page: a power of two from 16 to 65536                */
+  int32_t n_pages;   /* pages of the pool                                                */
+  int32_t max_pages; /* pages a sequence can have (columns of the page table); max_pages * page <= 2^30 */
+} pasa_cache_t;
+
+/* host-only.  Bytes of a pool: n_pages * H_kv * page * (d + 8 * d / group); 0 for an invalid description. */
+PASA_API size_t pasa_cache_bytes(const pasa_cache_t* cache);
+
+/* k, v: bf16 [B, H_kv, n, d] (shape strides), shape->H = H_kv.  Each call writes the bytes of its tokens and no others. */
+PASA_API int pasa_cache_write(const void* k, const void* v, const pasa_shape_t* shape, const pasa_cache_t* cache, void* pool, size_t pool_bytes,
+                              const int32_t* pages, const int32_t* len, const int32_t* n_new, void* stream);
+
+/* k, v: bf16 [B, H_kv, n, d] (shape strides, out): s c + m, rounded to binary32 and then to bf16. */
+PASA_API int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes, const int32_t* pages,
+                             const int32_t* len, const int32_t* n_new, void* k, void* v, void* stream);
+
+/*
+ * O = softmax(Q K^T * scale) V over the cached tokens t < len[b]; with causal != 0 a row sees the tokens up to and including its own
+ * only.  shape->H is a multiple of H_kv: head h attends over key/value head h / (H / H_kv).  A row that sees no token is zero, its lse -inf.
+ *   q, out  bf16 [B, H, n, d] (shape strides);  lse fp32 [B*H, n] or NULL
+ *   n_max   host: what len is expected not to exceed, 0 for max_pages * page.  The work is divided for this length; longer
+ *           sequences are computed as well, only more slowly.
+ *   ws      pasa_cache_attn_workspace_bytes(shape, cache, n_max) bytes (host-only helper; 0 on invalid arguments), 256-byte aligned.
+ *           It belongs to the call alone: calls that overlap in time need one each.
+ */
+PASA_API size_t pasa_cache_attn_workspace_bytes(const pasa_shape_t* shape, const pasa_cache_t* cache, int32_t n_max);
+PASA_API int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes,
+                             const int32_t* pages, const int32_t* len, const int32_t* n_new, int32_t causal, int32_t n_max, void* out, float* lse,
+                             void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Measurement aid (not part of the forward, cites nothing): launches `workgroups` workgroups of 256 threads that

@@ -6,6 +6,7 @@ points.  PyTorch is used for device memory and streams only.  There is no CPU fa
 entry point without the built library raises.
 """
 from .pasa import (  # noqa: F401
+    Cache,
     PasaError,
     Shape,
     attn_dense_ref,
@@ -14,6 +15,11 @@ from .pasa import (  # noqa: F401
     block_score,
     check_selection,
     budget_schedule,
+    cache_attn,
+    cache_attn_workspace_bytes,
+    cache_bytes,
+    cache_read,
+    cache_write,
     forward,
     forward_single_call,
     key_prior,

@@ -24,12 +24,13 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-int check_shape(const pasa_shape_t* s) {
+// blocks: whether the shape's block counts (the cache's entry points take row tensors only)
+int check_shape(const pasa_shape_t* s, bool blocks = true) {
   if (!s) return PASA_EINVAL;
   if (s->B < 1 || s->H < 1 || s->n < 1) return PASA_EINVAL;
   if ((int64_t)s->B * s->H > 65535) return PASA_EUNSUPPORTED;
   if (s->d != 64 && s->d != 128) return PASA_EUNSUPPORTED;
-  if (s->block != 64 && s->block != 128) return PASA_EUNSUPPORTED;
+  if (blocks && s->block != 64 && s->block != 128) return PASA_EUNSUPPORTED;
   if (!(s->scale >= 0.f) || isinf(s->scale)) return PASA_EINVAL;
   if (s->stride_n < s->d || s->stride_h < 1 || s->stride_b < 1) return PASA_EINVAL;
   if ((s->stride_n % 8) || (s->stride_h % 8) || (s->stride_b % 8)) return PASA_EALIGN;
@@ -723,6 +724,102 @@ int pasa_forward_buffers(const void* q, const void* k, const void* v, const pasa
 int pasa_attn_dense_ref(const void* q, const void* k, const void* v, const pasa_shape_t* shape, void* out, float* lse,
                         void* ws, size_t ws_bytes, void* stream) {
   return attn_common(q, k, v, shape, nullptr, nullptr, 0, out, lse, ws, ws_bytes, stream, false, false);
+}
+
+// ---- the 4-bit key/value cache -----------------------------------------------------------------------
+namespace {
+int check_cache(const pasa_cache_t* c) {
+  if (!c) return PASA_EINVAL;
+  if (c->H_kv < 1 || c->n_pages < 1 || c->max_pages < 1) return PASA_EINVAL;
+  if (c->d != 64 && c->d != 128) return PASA_EUNSUPPORTED;
+  if ((c->group != 32 && c->group != 64 && c->group != 128) || c->group > c->d) return PASA_EUNSUPPORTED;
+  if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1))) return PASA_EUNSUPPORTED;
+  if ((int64_t)c->max_pages * c->page > ((int64_t)1 << 30)) return PASA_EUNSUPPORTED;
+  if (c->H_kv > 65535 || (int64_t)c->n_pages * c->H_kv > ((int64_t)1 << 38)) return PASA_EUNSUPPORTED;  // bytes in 64 bits
+  return PASA_OK;
+}
+
+int64_t cache_head_bytes(const pasa_cache_t* c) { return (int64_t)c->page * (c->d + 8 * (c->d / c->group)); }
+
+// everything the three calls have in common
+int cache_params(const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes, const int32_t* pages, const int32_t* len,
+                 const int32_t* n_new, CacheParams* out) {
+  const int rc = check_shape(shape, /*blocks=*/false);
+  if (rc != PASA_OK) return rc;
+  const int rk = check_cache(cache);
+  if (rk != PASA_OK) return rk;
+  if (shape->d != cache->d) return PASA_EINVAL;
+  if (!pool || !pages || !len) return PASA_EINVAL;
+  if (!aligned16(pool) || !aligned4(pages) || !aligned4(len) || !aligned4(n_new)) return PASA_EALIGN;
+  if (pool_bytes < pasa_cache_bytes(cache)) return PASA_EWORKSPACE;
+  CacheParams& p = *out;
+  p.pool = static_cast<uint8_t*>(const_cast<void*>(pool));
+  p.pages = pages; p.len = len; p.n_new = n_new;
+  p.B = shape->B; p.H_kv = cache->H_kv; p.d = cache->d; p.group = cache->group;
+  p.log_page = __builtin_ctz((unsigned)cache->page);
+  p.n_pages = cache->n_pages; p.max_pages = cache->max_pages;
+  p.head_bytes = cache_head_bytes(cache);
+  return PASA_OK;
+}
+
+int cache_rows_params(const void* k, const void* v, const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes,
+                      const int32_t* pages, const int32_t* len, const int32_t* n_new, CacheRowsParams* out) {
+  CacheRowsParams& p = *out;
+  p = CacheRowsParams{};
+  const int rc = cache_params(shape, cache, pool, pool_bytes, pages, len, n_new, &p.c);
+  if (rc != PASA_OK) return rc;
+  if (shape->H != cache->H_kv) return PASA_EINVAL;
+  if (!k || !v) return PASA_EINVAL;
+  if (!aligned16(k) || !aligned16(v)) return PASA_EALIGN;
+  p.k = static_cast<uint16_t*>(const_cast<void*>(k)); p.v = static_cast<uint16_t*>(const_cast<void*>(v));
+  p.stride_b = shape->stride_b; p.stride_h = shape->stride_h; p.stride_n = shape->stride_n;
+  p.n = shape->n;
+  return PASA_OK;
+}
+}  // namespace
+
+size_t pasa_cache_bytes(const pasa_cache_t* cache) {
+  return check_cache(cache) != PASA_OK ? 0 : (size_t)cache->n_pages * cache->H_kv * (size_t)cache_head_bytes(cache);
+}
+
+int pasa_cache_write(const void* k, const void* v, const pasa_shape_t* shape, const pasa_cache_t* cache, void* pool, size_t pool_bytes,
+                     const int32_t* pages, const int32_t* len, const int32_t* n_new, void* stream) {
+  CacheRowsParams p;
+  const int rc = cache_rows_params(k, v, shape, cache, pool, pool_bytes, pages, len, n_new, &p);
+  if (rc != PASA_OK) return rc;
+  return pasa_launch_cache_write(p, static_cast<hipStream_t>(stream)) == hipSuccess ? PASA_OK : PASA_EHIP;
+}
+
+int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes, const int32_t* pages,
+                    const int32_t* len, const int32_t* n_new, void* k, void* v, void* stream) {
+  CacheRowsParams p;
+  const int rc = cache_rows_params(k, v, shape, cache, pool, pool_bytes, pages, len, n_new, &p);
+  if (rc != PASA_OK) return rc;
+  if (k == v) return PASA_EINVAL;
+  return pasa_launch_cache_read(p, static_cast<hipStream_t>(stream)) == hipSuccess ? PASA_OK : PASA_EHIP;
+}
+
+size_t pasa_cache_attn_workspace_bytes(const pasa_shape_t* shape, const pasa_cache_t* cache, int32_t n_max) {
+  if (check_shape(shape, false) != PASA_OK || check_cache(cache) != PASA_OK || n_max < 0) return 0;
+  if (shape->d != cache->d || shape->H % cache->H_kv) return 0;
+  return kAlign;
+}
+
+int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes, const int32_t* pages,
+                    const int32_t* len, const int32_t* n_new, int32_t causal, int32_t n_max, void* out, float* lse, void* ws, size_t ws_bytes,
+                    void* stream) {
+  CacheAttnParams p{};
+  const int rc = cache_params(shape, cache, pool, pool_bytes, pages, len, n_new, &p.c);
+  if (rc != PASA_OK) return rc;
+  if (shape->H % cache->H_kv || n_max < 0) return PASA_EINVAL;
+  if (!q || !out || !ws || out == q) return PASA_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned4(lse)) return PASA_EALIGN;
+  if (ws_bytes < pasa_cache_attn_workspace_bytes(shape, cache, n_max)) return PASA_EWORKSPACE;
+  p.q = static_cast<const uint16_t*>(q); p.o = static_cast<uint16_t*>(out); p.lse = lse;
+  p.stride_b = shape->stride_b; p.stride_h = shape->stride_h; p.stride_n = shape->stride_n;
+  p.H = shape->H; p.n = shape->n; p.causal = causal != 0;
+  p.scale = effective_scale(shape) * 1.4426950408889634f;
+  return pasa_launch_cache_attn(p, static_cast<hipStream_t>(stream)) == hipSuccess ? PASA_OK : PASA_EHIP;
 }
 
 }  // extern "C"

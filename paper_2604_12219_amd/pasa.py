@@ -18,7 +18,8 @@ _lib = None
 EXPORTS = ("pasa_strerror", "pasa_topk_count", "pasa_num_blocks", "pasa_mask_words", "pasa_score_workspace_bytes",
            "pasa_attn_workspace_bytes", "pasa_attn_variant", "pasa_block_score", "pasa_block_score_with_stats", "pasa_route", "pasa_route_gumbel", "pasa_kv_stats", "pasa_key_prior", "pasa_sparse_attn_fwd",
            "pasa_sparse_attn_fwd_prepared", "pasa_sparse_attn_fwd_static", "pasa_forward", "pasa_forward_buffers", "pasa_forward_workspace_bytes", "pasa_check_selection", "pasa_attn_dense_ref", "pasa_l1_workspace_bytes", "pasa_l1_distance",
-           "pasa_budget_schedule", "pasa_mfma_probe")
+           "pasa_budget_schedule", "pasa_mfma_probe", "pasa_cache_bytes", "pasa_cache_write", "pasa_cache_read", "pasa_cache_attn",
+           "pasa_cache_attn_workspace_bytes")
 
 
 class PasaError(RuntimeError):
@@ -60,6 +61,25 @@ class Shape:
     def c(self) -> _CShape:
         return _CShape(self.B, self.H, self.n, self.d, self.block, self.group, self.stride_b, self.stride_h,
                        self.stride_n, self.scale, self.kv_slices)
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [("H_kv", ctypes.c_int32), ("d", ctypes.c_int32), ("group", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+@dataclass
+class Cache:
+    """a key/value cache in 4 bits (pasa_cache_t): pages of `page` tokens, `n_pages` of them in the pool, at most `max_pages` a sequence"""
+    H_kv: int
+    d: int
+    n_pages: int
+    max_pages: int
+    group: int = 32
+    page: int = 64
+
+    def c(self) -> _CCache:
+        return _CCache(self.H_kv, self.d, self.group, self.page, self.n_pages, self.max_pages)
 
 
 def lib_path() -> str:
@@ -129,6 +149,17 @@ def load_library() -> ctypes.CDLL:
                                            ctypes.c_double, ctypes.POINTER(ctypes.c_double)]
         L.pasa_attn_dense_ref.restype = ctypes.c_int
         L.pasa_attn_dense_ref.argtypes = [vp, vp, vp, sp, vp, vp, vp, ctypes.c_size_t, vp]
+        cp = ctypes.POINTER(_CCache)
+        L.pasa_cache_bytes.restype = ctypes.c_size_t
+        L.pasa_cache_bytes.argtypes = [cp]
+        L.pasa_cache_write.restype = ctypes.c_int
+        L.pasa_cache_write.argtypes = [vp, vp, sp, cp, vp, ctypes.c_size_t, vp, vp, vp, vp]
+        L.pasa_cache_read.restype = ctypes.c_int
+        L.pasa_cache_read.argtypes = [sp, cp, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
+        L.pasa_cache_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.pasa_cache_attn_workspace_bytes.argtypes = [sp, cp, ctypes.c_int32]
+        L.pasa_cache_attn.restype = ctypes.c_int
+        L.pasa_cache_attn.argtypes = [vp, sp, cp, vp, ctypes.c_size_t, vp, vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -415,6 +446,79 @@ def forward_single_call(q, k, v, shape: Shape, keep_ratio: float, seed: int, noi
     _check_extent(shape, q=q, k=k, v=v, out=out)
     _check(L.pasa_forward(_ptr(q), _ptr(k), _ptr(v), c, float(keep_ratio), seed & (2**64 - 1), noise_amp,
                           _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream()), "pasa_forward")
+    return (out, lse) if want_lse else out
+
+
+def cache_bytes(cache: Cache) -> int:
+    """bytes of the pool of a cache"""
+    nbytes = load_library().pasa_cache_bytes(ctypes.byref(cache.c()))
+    if nbytes == 0:
+        raise ValueError(f"not a valid cache: {cache}")
+    return nbytes
+
+
+def cache_attn_workspace_bytes(shape: Shape, cache: Cache, n_max: int = 0) -> int:
+    return load_library().pasa_cache_attn_workspace_bytes(ctypes.byref(shape.c()), ctypes.byref(cache.c()), n_max)
+
+
+def _check_cache_args(shape: Shape, cache: Cache, pool, pages, length, n_new, rows: dict):
+    """what the library cannot see: types, sizes, layouts and devices of the tensors behind the pointers"""
+    want = (shape.B, shape.H, shape.n, shape.d)
+    for name, t in rows.items():
+        if tuple(t.shape) != want:
+            raise ValueError(f"{name}: expected {list(want)} as the shape says, got {list(t.shape)}")
+    _check_extent(shape, **rows)
+    _check_strides(shape, **rows)
+    if pool.dtype != torch.uint8 or not pool.is_contiguous():
+        raise ValueError("pool: expected a contiguous uint8 tensor")
+    for name, t, size in (("pages", pages, (shape.B, cache.max_pages)), ("length", length, (shape.B,)), ("n_new", n_new, (shape.B,))):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != size or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous int32 tensor of size {list(size)}")
+    here = torch.cuda.current_device() if pool.is_cuda else -1
+    for name, t in dict(rows, pool=pool, pages=pages, length=length, n_new=n_new).items():
+        if t is not None and (not t.is_cuda or t.get_device() != here):
+            raise ValueError(f"{name}: lies on {t.device}; every tensor has to be on the current GPU")
+
+
+def cache_write(k, v, shape: Shape, cache: Cache, pool, pages, length, n_new=None):
+    """quantises row i < n_new[b] of k, v [B, H_kv, n, d] into the cache as token length[b] - n_new[b] + i of sequence b (n_new None: all n
+    rows).  pool uint8 [cache_bytes(cache)], pages int32 [B, max_pages], length and n_new int32 [B], see pasa.h"""
+    _check_cache_args(shape, cache, pool, pages, length, n_new, {"k": k, "v": v})
+    _check(load_library().pasa_cache_write(_ptr(k), _ptr(v), ctypes.byref(shape.c()), ctypes.byref(cache.c()), _ptr(pool), pool.numel(), _ptr(pages),
+                                           _ptr(length), _ptr(n_new), _stream()), "pasa_cache_write")
+
+
+def cache_read(shape: Shape, cache: Cache, pool, pages, length, n_new=None, k=None, v=None):
+    """-> (k, v) bf16 [B, H_kv, n, d]: row i < n_new[b] is token length[b] - n_new[b] + i of sequence b as the cache holds it.  Other rows keep what
+    they held (new tensors: zero)"""
+    if k is None or v is None:
+        full = torch.zeros((2, shape.B, shape.H, shape.n, shape.d), dtype=torch.bfloat16, device=pool.device)
+        k, v = (full[0] if k is None else k), (full[1] if v is None else v)
+    _check_cache_args(shape, cache, pool, pages, length, n_new, {"k": k, "v": v})
+    _check(load_library().pasa_cache_read(ctypes.byref(shape.c()), ctypes.byref(cache.c()), _ptr(pool), pool.numel(), _ptr(pages), _ptr(length),
+                                          _ptr(n_new), _ptr(k), _ptr(v), _stream()), "pasa_cache_read")
+    return k, v
+
+
+def cache_attn(q, shape: Shape, cache: Cache, pool, pages, length, n_new=None, causal: bool = False, n_max: int = 0, out=None, lse=None, ws=None,
+               want_lse: bool = False):
+    """attention of the new rows q [B, H, n, d] over the cached tokens of their sequences (causal: up to a row's own token).  n_max: what
+    length is expected not to exceed (host; 0: what the page table can hold).  Rows at and behind n_new[b] of out and lse are
+    left alone (new tensors: zero)"""
+    if out is None:
+        out = torch.zeros_like(q)
+    if lse is None and want_lse:
+        lse = torch.zeros((shape.B * shape.H, shape.n), dtype=torch.float32, device=q.device)
+    _check_cache_args(shape, cache, pool, pages, length, n_new, {"q": q, "out": out})
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != shape.B * shape.H * shape.n or not lse.is_contiguous() or
+                            lse.get_device() != q.get_device()):
+        raise ValueError(f"lse: expected a contiguous fp32 tensor of size {[shape.B * shape.H, shape.n]} beside q")
+    ws = _workspace(lambda: cache_attn_workspace_bytes(shape, cache, n_max), q.device, ws)
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.get_device() != q.get_device():
+        raise ValueError("ws: expected a contiguous uint8 tensor beside q")
+    _check(load_library().pasa_cache_attn(_ptr(q), ctypes.byref(shape.c()), ctypes.byref(cache.c()), _ptr(pool), pool.numel(), _ptr(pages),
+                                          _ptr(length), _ptr(n_new), int(causal), n_max, _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream()),
+           "pasa_cache_attn")
     return (out, lse) if want_lse else out
 
 
