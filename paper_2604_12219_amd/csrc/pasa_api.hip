@@ -776,6 +776,27 @@ int cache_rows_params(const void* k, const void* v, const pasa_shape_t* shape, c
   p.n = shape->n;
   return PASA_OK;
 }
+// the rows of a key/value head's query heads are numbered in 32 bits, with room for a last incomplete workgroup and for the splits
+bool cache_rows_fit(const pasa_shape_t* s, const pasa_cache_t* c) { return (int64_t)(s->H / c->H_kv) * s->n <= ((int64_t)1 << 30); }
+
+// How the rows and tokens of a call are divided among workgroups, and the workspace that takes
+struct CacheAttnPlan {
+  int wg_rows, splits;
+  size_t part_ml, total;
+};
+CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int32_t n_max) {
+  CacheAttnPlan a{};
+  const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
+  const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
+  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+  const int64_t wgs = (int64_t)s->B * c->H_kv * ((rows + a.wg_rows - 1) / a.wg_rows);
+  a.splits = 1;
+  while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= 768 && tokens >= (a.splits + 1) * 512) ++a.splits;
+  const size_t parts = a.splits > 1 ? (size_t)s->B * s->H * s->n * a.splits : 0;
+  a.part_ml = align_up(parts * s->d * 4);
+  a.total = align_up(a.part_ml + parts * 2 * 4 + 1);  // never zero: that means "invalid"
+  return a;
+}
 }  // namespace
 
 size_t pasa_cache_bytes(const pasa_cache_t* cache) {
@@ -801,8 +822,8 @@ int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cache, const 
 
 size_t pasa_cache_attn_workspace_bytes(const pasa_shape_t* shape, const pasa_cache_t* cache, int32_t n_max) {
   if (check_shape(shape, false) != PASA_OK || check_cache(cache) != PASA_OK || n_max < 0) return 0;
-  if (shape->d != cache->d || shape->H % cache->H_kv) return 0;
-  return kAlign;
+  if (shape->d != cache->d || shape->H % cache->H_kv || !cache_rows_fit(shape, cache)) return 0;
+  return cache_attn_plan(shape, cache, n_max).total;
 }
 
 int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes, const int32_t* pages,
@@ -812,13 +833,18 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   const int rc = cache_params(shape, cache, pool, pool_bytes, pages, len, n_new, &p.c);
   if (rc != PASA_OK) return rc;
   if (shape->H % cache->H_kv || n_max < 0) return PASA_EINVAL;
+  if (!cache_rows_fit(shape, cache)) return PASA_EUNSUPPORTED;
   if (!q || !out || !ws || out == q) return PASA_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned4(lse)) return PASA_EALIGN;
-  if (ws_bytes < pasa_cache_attn_workspace_bytes(shape, cache, n_max)) return PASA_EWORKSPACE;
+  const CacheAttnPlan plan = cache_attn_plan(shape, cache, n_max);
+  if (ws_bytes < plan.total) return PASA_EWORKSPACE;
   p.q = static_cast<const uint16_t*>(q); p.o = static_cast<uint16_t*>(out); p.lse = lse;
   p.stride_b = shape->stride_b; p.stride_h = shape->stride_h; p.stride_n = shape->stride_n;
   p.H = shape->H; p.n = shape->n; p.causal = causal != 0;
   p.scale = effective_scale(shape) * 1.4426950408889634f;
+  p.wg_rows = plan.wg_rows; p.splits = plan.splits;
+  p.part_o = static_cast<float*>(ws);
+  p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.part_ml);
   return pasa_launch_cache_attn(p, static_cast<hipStream_t>(stream)) == hipSuccess ? PASA_OK : PASA_EHIP;
 }
 
