@@ -173,15 +173,14 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
   uint32_t kc[4][NW], kp[4][NG], vc[4][NW], vp[4][NG];
   const uint8_t* run[4];
   uint32_t slot[4];
-  uint32_t followed, next_followed = 0u;  // bit t: the page of sub-tile t is one
+  int key0[4];  // position of the sub-tile's first token; beyond every limit if its page is not followed
   auto find = [&](int tile) {
-    next_followed = 0u;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int pos = 64 * tile + 16 * t;
       const int pg = table[min(pos, seq.length - 1) >> p.c.log_page];  // (behind the last token: masked, but some page of the sequence)
       const bool ok = pg >= 0 && pg < p.c.n_pages;
-      next_followed |= (uint32_t)ok << t;
+      key0[t] = ok ? pos : 0x7fffff00;
       run[t] = p.c.pool + ((int64_t)(ok ? pg : 0) * p.c.H_kv + hkv) * p.c.head_bytes;
       slot[t] = (uint32_t)pos & (page - 1u);
     }
@@ -209,8 +208,14 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
   const uint8_t* const v_read = vl + v_token * L::CODE;
   const int w_row = (col >> 2) * NR + min(col & 3, NR - 1);  // the row of slot col (or, unused slots, any)
 
-  auto tile_step = [&](int tile, auto masked) {
-    constexpr bool MASKED = decltype(masked)::value;
+  int tile = split * per + wave;
+  if (tile < t_end) {
+    find(tile);
+    load_v();
+    load_k();
+    load_vp();
+  }
+  for (; tile < t_end; tile += kWaves) {
     wave_fence();
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -218,11 +223,14 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
       if constexpr (NW == 4) *reinterpret_cast<uint4*>(at) = make_uint4(vc[t][0], vc[t][1], vc[t][2], vc[t][3]);
       else *reinterpret_cast<uint2*>(at) = make_uint2(vc[t][0], vc[t][1]);
     }
-    const bool more = tile + kWaves < t_end;
-    if (more) {
-      find(tile + kWaves);
-      load_v();
-    }
+    int key[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) key[t] = key0[t] + col;
+    const bool whole = max(max(key0[0], key0[1]), max(key0[2], key0[3])) + 16 <= limit_all;  // every row sees every token
+    // Every operand of the next tile is requested where this tile's is used up, most of a step ahead.  (The last step requests
+    // its own tile again: requests under a condition cost the compiler copies of all these registers.)
+    find(tile + kWaves < t_end ? tile + kWaves : tile);
+    load_v();
     float s[4][NR];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -235,19 +243,16 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
 #pragma unroll
         for (int i = 0; i < NR; ++i) s[t][i] = fmaf(sc, acc[i], g == 0 ? mn * qsum[g][i] : fmaf(mn, qsum[g][i], s[t][i]));
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (more) load_k();
-    if constexpr (MASKED) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-          if (64 * tile + 16 * t + col >= limit[i] || !((followed >> t) & 1u)) s[t][i] = -INFINITY;
-    }
+    load_k();
+    __builtin_amdgcn_sched_barrier(0);
     float mx[NR];
     bool grows = false;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t][i] = key[t] < limit[i] ? s[t][i] : -INFINITY;
       mx[i] = row16_max(fmaxf(fmaxf(s[0][i], s[1][i]), fmaxf(s[2][i], s[3][i]))) * p.scale;
       grows |= mx[i] > m[i];
     }
@@ -273,33 +278,37 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
         l[i] += s[t][i];
       }
     }
+    auto weights = [&](auto masked) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      float sc[4], mm[4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        sc[t] = bf16_low(vp[t][g]);
-        mm[t] = fmaf(7.5f, sc[t], bf16_high(vp[t][g]));
-      }
-#pragma unroll
-      for (int i = 0; i < NR; ++i) {
-        bf16x8 w;  // (the upper half unused)
+      for (int g = 0; g < NG; ++g) {
+        float sc[4], mm[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          float ps = s[t][i] * sc[t], pm = s[t][i] * mm[t];
-          if constexpr (MASKED) {  // a token that is not seen may have any parameters, NaN among them
-            const bool seen = 64 * tile + 16 * t + col < limit[i] && ((followed >> t) & 1u);
-            ps = seen ? ps : 0.f;
-            pm = seen ? pm : 0.f;
-          }
-          w[t] = (__bf16)ps;
-          mid[g][i] += pm;
+          sc[t] = bf16_low(vp[t][g]);
+          mm[t] = fmaf(7.5f, sc[t], bf16_high(vp[t][g]));
         }
-        const u32x4 bits = __builtin_bit_cast(u32x4, w);
-        *reinterpret_cast<uint2*>(&sh.work.w[wave][g][x * NR + i][4 * col]) = make_uint2(bits[0], bits[1]);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          bf16x8 w;  // (the upper half unused)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            float ps = s[t][i] * sc[t], pm = s[t][i] * mm[t];
+            if constexpr (decltype(masked)::value) {  // a token that is not seen may have any parameters, NaN among them
+              ps = key[t] < limit[i] ? ps : 0.f;
+              pm = key[t] < limit[i] ? pm : 0.f;
+            }
+            w[t] = (__bf16)ps;
+            mid[g][i] += pm;
+          }
+          const u32x4 bits = __builtin_bit_cast(u32x4, w);
+          *reinterpret_cast<uint2*>(&sh.work.w[wave][g][x * NR + i][4 * col]) = make_uint2(bits[0], bits[1]);
+        }
       }
-    }
-    if (more) load_vp();
+    };
+    if (whole) weights(std::false_type{});
+    else weights(std::true_type{});
+    load_vp();
+    __builtin_amdgcn_sched_barrier(0);
     wave_fence();
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -313,20 +322,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
         o[c] = mfma16(w0, codes_bf16((uint32_t)v[0]), o[c]);
         o[c] = mfma16(w1, codes_bf16((uint32_t)v[1]), o[c]);
       }
-    }
-    followed = next_followed;
-  };
-
-  int tile = split * per + wave;
-  if (tile < t_end) {
-    find(tile);
-    followed = next_followed;
-    load_v();
-    load_k();
-    load_vp();
-    for (; tile < t_end; tile += kWaves) {
-      if (64 * tile + 64 <= limit_all && followed == 15u) tile_step(tile, std::false_type{});
-      else tile_step(tile, std::true_type{});
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
