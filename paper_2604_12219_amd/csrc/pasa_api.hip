@@ -788,10 +788,11 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   CacheAttnPlan a{};
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
-  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 32 ? 16 : rows <= 128 ? 128 : 256;
+  const int64_t resident = a.wg_rows <= 16 ? 768 : a.wg_rows == 128 ? 512 : 256;
   const int64_t wgs = (int64_t)s->B * c->H_kv * ((rows + a.wg_rows - 1) / a.wg_rows);
   a.splits = 1;
-  while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= 768 && tokens >= (a.splits + 1) * 512) ++a.splits;
+  while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= resident && tokens >= (a.splits + 1) * 512) ++a.splits;
   const size_t parts = a.splits > 1 ? (size_t)s->B * s->H * s->n * a.splits : 0;
   a.part_ml = align_up(parts * s->d * 4);
   a.total = align_up(a.part_ml + parts * 2 * 4 + 1);  // never zero: that means "invalid"

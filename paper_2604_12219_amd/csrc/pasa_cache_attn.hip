@@ -399,19 +399,28 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttnParams p) {
 }
 
 template <int D, int G>
-hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
+hipError_t launch_rows(const CacheAttnParams& p, hipStream_t stream) {
   const int rows = p.H / p.c.H_kv * p.n;
   const dim3 grid((rows + p.wg_rows - 1) / p.wg_rows * p.splits, p.c.H_kv, p.c.B);
   if (p.wg_rows == 4) cache_rows_kernel<D, G, 1><<<grid, kWaves * 64, 0, stream>>>(p);
   else if (p.wg_rows == 8) cache_rows_kernel<D, G, 2><<<grid, kWaves * 64, 0, stream>>>(p);
   else cache_rows_kernel<D, G, 4><<<grid, kWaves * 64, 0, stream>>>(p);
-  if (p.splits > 1) cache_merge_kernel<D><<<dim3((p.n + 3) / 4, p.H, p.c.B), 256, 0, stream>>>(p);
   return hipGetLastError();
+}
+
+hipError_t launch_rows(const CacheAttnParams& p, hipStream_t stream) {
+  if (p.c.d == 64) return p.c.group == 32 ? launch_rows<64, 32>(p, stream) : launch_rows<64, 64>(p, stream);
+  return p.c.group == 32 ? launch_rows<128, 32>(p, stream)
+       : p.c.group == 64 ? launch_rows<128, 64>(p, stream) : launch_rows<128, 128>(p, stream);
 }
 
 }  // namespace
 
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream) {
-  if (p.c.d == 64) return p.c.group == 32 ? launch<64, 32>(p, stream) : launch<64, 64>(p, stream);
-  return p.c.group == 32 ? launch<128, 32>(p, stream) : p.c.group == 64 ? launch<128, 64>(p, stream) : launch<128, 128>(p, stream);
+  const hipError_t rc = p.wg_rows >= 128 ? pasa_launch_cache_tiles(p, stream) : launch_rows(p, stream);
+  if (rc != hipSuccess || p.splits == 1) return rc;
+  const dim3 grid((p.n + 3) / 4, p.H, p.c.B);
+  if (p.c.d == 64) cache_merge_kernel<64><<<grid, 256, 0, stream>>>(p);
+  else cache_merge_kernel<128><<<grid, 256, 0, stream>>>(p);
+  return hipGetLastError();
 }

@@ -1,0 +1,290 @@
+// Attention of many new rows over the 4-bit cache: the matrix-core side of pasa_cache_attn.hip.
+//
+// Bound by the matrix cores, as attention over bf16 is, so the tiles are what that uses: 64 tokens of K and V in bf16 in LDS, and the
+// instruction streams of pasa_mfma_pipes.hpp over them.  What differs is how a tile gets there: a thread holds one token's codes of a quarter
+// of its channels, K or V, makes bf16 of them and writes them to the other half of the ring while this tile is worked on.  That
+// costs 2.5 vector instructions a value: a shift and an and-or put two codes into fp16 numbers 1 + c/16, a mixed fma makes s c + m of each
+// (16 s (1 + c/16) + (m - 16 s), whose rounding is 2^-20 of s), a conversion rounds two of them to bf16, the type of the matrix
+// operands.  Values are shared by all rows of a workgroup, so the wider one (eight waves, 256 rows) pays half as much a row.
+#include "pasa_cache.hpp"
+#include "pasa_mfma_pipes.hpp"
+
+#include <type_traits>
+
+namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+typedef __attribute__((address_space(4))) const int32_t const_i32;
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// 8 values of a word of codes in bf16; a = 16 s, b = m - 16 s
+PASA_DEVICE uint4 values8(uint32_t x, float a, float b) {
+  const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 2) & 0x03c003c0u) | 0x3c003c00u,
+                         ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
+  float lo[4], hi[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // channels i and i + 4
+    const f16x2 c = __builtin_bit_cast(f16x2, h[i]);
+    lo[i] = fmaf((float)c[0], a, b);
+    hi[i] = fmaf((float)c[1], a, b);
+  }
+  const bf16x2 r[4] = {{(__bf16)lo[0], (__bf16)lo[1]}, {(__bf16)lo[2], (__bf16)lo[3]}, {(__bf16)hi[0], (__bf16)hi[1]}, {(__bf16)hi[2], (__bf16)hi[3]}};
+  return make_uint4(__builtin_bit_cast(uint32_t, r[0]), __builtin_bit_cast(uint32_t, r[1]), __builtin_bit_cast(uint32_t, r[2]), __builtin_bit_cast(uint32_t, r[3]));
+}
+
+template <int N>
+PASA_DEVICE void load_words(const uint8_t* at, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(at);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    static_assert(N == 1, "");
+    w[0] = *reinterpret_cast<const uint32_t*>(at);
+  }
+}
+
+PASA_DEVICE bool finite_param(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
+
+// One token's share of a tile: a quarter of its K (or V) codes, and the parameters that they need
+template <int D, int G, bool KEY>
+struct TokenPart {
+  typedef CacheLayout<D, G> L;
+  static constexpr int NW = D / 32, NP = KEY ? D / G : 1;
+  uint32_t code[NW], par[NP];
+  uint32_t v_par[KEY ? D / G : 1];  // K of a tile that not every row sees whole: the token's V parameters
+  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, int quarter, bool whole) {
+    load_words<NW>(run + (KEY ? L::k_codes(page) : L::v_codes(page)) + slot * L::CODE + quarter * (L::CODE / 4), code);
+    if constexpr (KEY) {
+      load_words<NP>(run + L::k_params(page) + slot * L::PARAM, par);
+      if (!whole) load_words<NP>(run + L::v_params(page) + slot * L::PARAM, v_par);
+    } else {
+      load_words<1>(run + L::v_params(page) + slot * L::PARAM + 4 * (quarter * (D / 4) / G), par);
+    }
+  }
+  // Row `token` of the tile at `tile`.  Not every row of the workgroup sees every token of it (whole == false): weights of zero do not
+  // hide values that are not finite, so those leave V as zeros and make the token's keys NaN instead, which the rows that do not see
+  // it replace.  (A row that does see it is NaN throughout then, not only in the channels of that group.)  there: some row sees the token
+  PASA_DEVICE void store(char* tile, int token, int quarter, bool whole, bool there) const {
+    if constexpr (KEY) {
+      bool poison = false;
+      if (!whole) {
+#pragma unroll
+        for (int g = 0; g < NP; ++g) poison |= !finite_param(v_par[g]);
+      }
+#pragma unroll
+      for (int j = 0; j < NW; ++j) {
+        const uint32_t w = poison ? 0x7fc07fc0u : par[j * 32 / G];
+        const float s = bf16_low(w), a = 16.f * s;
+        *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, 4 * j + quarter)) = values8(code[j], a, bf16_high(w) - a);
+      }
+    } else {
+      const uint32_t w = whole || (there && finite_param(par[0])) ? par[0] : 0u;
+      const float s = bf16_low(w), a = 16.f * s, b = bf16_high(w) - a;
+#pragma unroll
+      for (int j = 0; j < NW; ++j) *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, quarter * NW + j)) = values8(code[j], a, b);
+    }
+  }
+};
+
+template <int D, int G, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnParams p) {
+  constexpr int ROWS = WAVES * 32, TILE = 64 * 2 * D;
+  constexpr bool BOTH = WAVES == 4;  // a thread has K and V of its token part; with eight waves four of them have K, four V
+  __shared__ __attribute__((aligned(1024))) char ring[4 * TILE];  // K, V of one tile, K, V of the next
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
+
+  // the last rows first: with a causal mask they have the most to do
+  const int row_tiles = gridDim.x / p.splits;
+  const int split = blockIdx.x % p.splits, row0 = (row_tiles - 1 - (int)(blockIdx.x / p.splits)) * ROWS, hkv = blockIdx.y, b = blockIdx.z;
+  const CacheSequence seq = cache_sequence(p.c, b, p.n);
+  const int share = p.H / p.c.H_kv, rows = share * seq.rows;
+  if (row0 >= rows) return;
+  const int last_row = min(row0 + ROWS, rows) - 1;
+  auto limit_of = [&](int r) -> int {  // tokens that row r sees
+    if (!p.causal) return seq.length;
+    const int64_t own = seq.first + r / share + 1;
+    return own < 0 ? 0 : own < seq.length ? (int)own : seq.length;
+  };
+  const int limit_all = __builtin_amdgcn_readfirstlane(limit_of(row0)), limit_any = __builtin_amdgcn_readfirstlane(limit_of(last_row));
+  const int tiles = (limit_any + 63) >> 6, per = (tiles + p.splits - 1) / p.splits;
+  const int t_begin = __builtin_amdgcn_readfirstlane(split * per), t_end = __builtin_amdgcn_readfirstlane(min(tiles, (split + 1) * per));
+  const uint32_t page = 1u << p.c.log_page;
+  const_i32* const table = (const_i32*)(p.c.pages + (int64_t)b * p.c.max_pages);
+
+  // this wave's rows, a lane's row in either half-wave
+  const int row = row0 + wave * 32 + ql;
+  const bool busy = row0 + wave * 32 <= last_row;  // (wave-uniform)
+  const int own = min(row, last_row), i_own = own / share, h_own = hkv * share + own % share;
+  const int64_t row_off = b * p.stride_b + h_own * p.stride_h + i_own * p.stride_n;
+  const int limit = limit_of(own);
+  bf16x8 qf[D / 16];
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p.q + row_off + 16 * s + 8 * h));
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) o[t] = f32x16{0};
+  float m = -INFINITY, l = 0.f;
+
+  const uint32_t ring_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+  uint32_t k_read = ring_base + (uint32_t)lds_chunk_off<D>(ql, h), v_read[2];
+  {
+    const int i = lane & 15, r = 4 * h + (i >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+    v_read[0] = ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r, c >> 3) + (c & 7) * 2);
+    v_read[1] = ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r + 8, c >> 3) + (c & 7) * 2);
+  }
+
+  // ---- how a tile gets into LDS ----
+  const int token = (tid & 255) >> 2, quarter = tid & 3;
+  const bool has_k = BOTH || wave < 4, has_v = BOTH || wave >= 4;
+  TokenPart<D, G, true> kt;
+  TokenPart<D, G, false> vt;
+  bool in_page = false;  // of the token part that is loaded: its page is followed
+  auto followed = [&](int tile) -> uint32_t {  // bit t: the page of tokens 64 tile + 16 t .. is followed
+    uint32_t bits = 0u;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int pg = table[min(64 * tile + 16 * t, seq.length - 1) >> p.c.log_page];
+      bits |= (uint32_t)(pg >= 0 && pg < p.c.n_pages) << t;
+    }
+    return bits;
+  };
+  auto is_whole = [&](int tile) -> bool { return 64 * tile + 64 <= limit_all && followed(tile) == 15u; };
+  auto load = [&](int tile, bool whole) {
+    const int pos = 64 * tile + token;
+    const int pg = p.c.pages[(int64_t)b * p.c.max_pages + (min(pos, seq.length - 1) >> p.c.log_page)];
+    const bool ok = pg >= 0 && pg < p.c.n_pages;
+    in_page = ok && pos < limit_any;
+    const uint8_t* const run = p.c.pool + ((int64_t)(ok ? pg : 0) * p.c.H_kv + hkv) * p.c.head_bytes;
+    const uint32_t slot = (uint32_t)pos & (page - 1u);
+    if (has_k) kt.load(run, page, slot, quarter, whole);
+    if (has_v) vt.load(run, page, slot, quarter, whole);
+  };
+  auto store = [&](int pair, bool whole) {
+    char* const at = ring + pair * 2 * TILE;
+    if (has_k) kt.store(at, token, quarter, whole, in_page);
+    if (has_v) vt.store(at + TILE, token, quarter, whole, in_page);
+  };
+
+  // ---- one tile ----
+  auto compute = [&](int tile, int pair, bool whole) {
+    const uint32_t off = (uint32_t)(pair * 2 * TILE);
+    f32x16 s0, s1;
+    bf16x8 pf[4];
+    pipes::rows_x_q(k_read + off, qf, s0, s1);
+    if (!whole) {
+      const int rel = limit - 64 * tile - 4 * h;
+      const uint32_t bits = followed(tile);
+      int lim[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) lim[t] = (bits >> t) & 1u ? rel : -64;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = mfma_row(r, 0);
+        if (key >= lim[r >> 3]) s0[r] = -INFINITY;
+        if (key + 32 >= lim[2 + (r >> 3)]) s1[r] = -INFINITY;
+      }
+    }
+    float mx = fmaxf(s0[0], s1[0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, s0[r]), s1[r]);
+    mx = half_swap_max(mx) * p.scale;
+    if (__builtin_amdgcn_ballot_w64(mx > m)) {
+      const float m_new = fmaxf(m, mx);
+      const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= corr;
+    }
+    const float neg = m == -INFINITY ? 0.f : -m;  // nothing seen yet: every weight is exp2(-inf) = 0
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s0[r] = __builtin_amdgcn_exp2f(fmaf(s0[r], p.scale, neg));
+      s1[r] = __builtin_amdgcn_exp2f(fmaf(s1[r], p.scale, neg));
+      sum += s0[r] + s1[r];
+    }
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {  // the weights to bf16, the type of the matrix operands
+      pf[0][i] = (__bf16)s0[i];
+      pf[1][i] = (__bf16)s0[8 + i];
+      pf[2][i] = (__bf16)s1[i];
+      pf[3][i] = (__bf16)s1[8 + i];
+    }
+    pipes::cols_x_p64(v_read[0] + off, v_read[1] + off, pf, o);
+  };
+
+  if (t_begin < t_end) {
+    bool whole = is_whole(t_begin), next_whole = t_begin + 1 < t_end && is_whole(t_begin + 1);
+    load(t_begin, whole);
+    store(0, whole);
+    if (t_begin + 1 < t_end) load(t_begin + 1, next_whole);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int tile = t_begin; tile < t_end; ++tile) {
+      const int pair = (tile - t_begin) & 1;
+      const bool more = tile + 1 < t_end, more2 = tile + 2 < t_end;
+      const bool after_whole = more2 && is_whole(tile + 2);
+      // Half of the waves convert the next tile before their matrix work, half of them after it: a SIMD has one of either
+      const bool first = (wave & 4) == 0;
+      if (first && more) {
+        store(pair ^ 1, next_whole);
+        if (more2) load(tile + 2, after_whole);
+      }
+      if (busy) compute(tile, pair, whole);
+      if (!first && more) {
+        store(pair ^ 1, next_whole);
+        if (more2) load(tile + 2, after_whole);
+      }
+      whole = next_whole;
+      next_whole = after_whole;
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+  }
+
+  l = half_swap_sum(l);
+  if (row > last_row) return;
+  const int64_t line = ((int64_t)b * p.H + h_own) * p.n + i_own;
+  if (p.splits == 1) {  // a row that sees nothing is zero, its normaliser empty
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const bf16x2 x0 = {(__bf16)(o[t][4 * g] * inv), (__bf16)(o[t][4 * g + 1] * inv)};
+        const bf16x2 x1 = {(__bf16)(o[t][4 * g + 2] * inv), (__bf16)(o[t][4 * g + 3] * inv)};
+        *reinterpret_cast<uint2*>(p.o + row_off + 32 * t + 8 * g + 4 * h) = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+      }
+    if (p.lse && h == 0) p.lse[line] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  } else {
+    const int64_t part = line * p.splits + split;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(p.part_o + part * D + 32 * t + 8 * g + 4 * h) = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
+    if (h == 0) { p.part_ml[2 * part] = m; p.part_ml[2 * part + 1] = l; }
+  }
+}
+
+template <int D, int G>
+hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
+  const int rows = p.H / p.c.H_kv * p.n;
+  const dim3 grid((rows + p.wg_rows - 1) / p.wg_rows * p.splits, p.c.H_kv, p.c.B);
+  if (p.wg_rows == 128) cache_tile_kernel<D, G, 4><<<grid, 256, 0, stream>>>(p);
+  else cache_tile_kernel<D, G, 8><<<grid, 512, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream) {
+  if (p.c.d == 64) return p.c.group == 32 ? launch<64, 32>(p, stream) : launch<64, 64>(p, stream);
+  return p.c.group == 32 ? launch<128, 32>(p, stream) : p.c.group == 64 ? launch<128, 64>(p, stream) : launch<128, 128>(p, stream);
+}

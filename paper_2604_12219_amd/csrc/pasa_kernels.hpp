@@ -134,10 +134,11 @@ struct CacheAttnParams {
   int64_t stride_b, stride_h, stride_n;
   int32_t H, n, causal;
   float scale;  // of the logits, times log2(e)
-  int32_t wg_rows;  // (row, head of a key/value head's share) pairs of a workgroup: 4, 8 or 16
+  int32_t wg_rows;  // (row, head of a key/value head's share) pairs of a workgroup: 4, 8, 16 (pasa_cache_attn.hip), 128 or 256 (pasa_cache_tile.hip)
   int32_t splits;   // workgroups among which a sequence's tokens are divided, at most kCacheMaxSplits
   float* part_o;    // splits > 1: fp32 [B][H][n][splits][d], sums against the maximum of their split
   float* part_ml;   //             fp32 [B][H][n][splits][2], that maximum (log2 units) and the sum of the weights
 };
 constexpr int kCacheMaxSplits = 64;  // a wave of the merging kernel holds one per lane
+hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // the attention kernel alone
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);
