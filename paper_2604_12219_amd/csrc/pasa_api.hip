@@ -1,6 +1,7 @@
 // C ABI of the PASA forward (see include/pasa.h): argument validation, workspace carving, launches.
 // Nothing here allocates, frees or synchronises.
 #include "pasa.h"
+#include "pasa_cache_kernels.hpp"
 #include "pasa_kernels.hpp"
 
 #include <math.h>

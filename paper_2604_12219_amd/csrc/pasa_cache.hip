@@ -8,6 +8,7 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr uint32_t kMostKey = 0x46800000u, kMostValue = 0x7f7fffffu;  // 16384; any finite number
 
 template <int CTRL>
 PASA_DEVICE float dpp_f(float x) {
@@ -27,11 +28,12 @@ PASA_DEVICE uint32_t bf16_round(float x) {  // to nearest, ties to even; x is fi
 // The codes and the parameter word of 8 channels (four words of bf16 pairs) whose group is the G/8 lanes around this one.
 //   s = bf16(binary32((max - min) / 15)), 0 below 2^-126;  code = nearest integer to (x - min) / s, ties to even
 // with the real quotients: binary32 decides where its error cannot matter, the rest is done over in 64 bits.
+// most: the largest bit pattern of |x| that can be held
 template <int G>
-PASA_DEVICE uint32_t quantise8(const uint4& raw, uint32_t& param) {
+PASA_DEVICE uint32_t quantise8(const uint4& raw, uint32_t& param, uint32_t most) {
   const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
   float x[8];
-  uint32_t top = 0u;  // largest |x| as a bit pattern: 0x7f80 and above are infinities and NaN
+  uint32_t top = 0u;  // largest |x| as a bit pattern (infinities and NaN are larger than any number)
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = bf16_low(w[i]);
@@ -52,7 +54,7 @@ PASA_DEVICE uint32_t quantise8(const uint4& raw, uint32_t& param) {
   if constexpr (G >= 128) {
     lo = fminf(lo, dpp_f<kMirror>(lo)); hi = fmaxf(hi, dpp_f<kMirror>(hi)); top = max(top, dpp_u<kMirror>(top));
   }
-  if (top >= 0x7f800000u) {  // the whole group reads back as NaN
+  if (top > most) {  // the whole group reads back as NaN
     param = 0x7fc07fc0u;
     return 0u;
   }
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(CacheRowsParams p
   const uint4 kr = *reinterpret_cast<const uint4*>(p.k + a.row_off + 8 * chunk);
   const uint4 vr = *reinterpret_cast<const uint4*>(p.v + a.row_off + 8 * chunk);
   uint32_t kp, vp;
-  const uint32_t kc = quantise8<G>(kr, kp), vc = quantise8<G>(vr, vp);
+  const uint32_t kc = quantise8<G>(kr, kp, kMostKey), vc = quantise8<G>(vr, vp, kMostValue);
   *reinterpret_cast<uint32_t*>(a.run + L::k_codes(page) + a.slot * L::CODE + 4 * k_word<D>(chunk)) = kc;
   *reinterpret_cast<uint32_t*>(a.run + L::v_codes(page) + a.slot * L::CODE + 4 * chunk) = vc;
   if (chunk % (G / 8) == 0) {

@@ -7,8 +7,8 @@
 // 8w .. 8w+7.  K word q * (d/32) + j holds the channels 32j + 8q .. + 7: the d/32 words of one q are one load, and each of
 // them lies in another run of 32 channels, so that a matrix instruction over one word per lane stays inside a group.
 #pragma once
+#include "pasa_cache_kernels.hpp"
 #include "pasa_device.hpp"
-#include "pasa_kernels.hpp"
 
 PASA_DEVICE float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 PASA_DEVICE float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

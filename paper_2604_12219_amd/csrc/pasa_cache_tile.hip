@@ -1,12 +1,19 @@
 // Attention of many new rows over the 4-bit cache: the matrix-core side of pasa_cache_attn.hip.
 //
-// Bound by the matrix cores, as attention over bf16 is, so the tiles are what that uses: 64 tokens of K and V in bf16 in LDS, and the
-// instruction streams of pasa_mfma_pipes.hpp over them.  What differs is how a tile gets there: a thread holds one token's codes of a quarter
-// of its channels, K or V, makes bf16 of them and writes them to the other half of the ring while this tile is worked on.  That
-// costs 2.5 vector instructions a value: a shift and an and-or put two codes into fp16 numbers 1 + c/16, a mixed fma makes s c + m of each
-// (16 s (1 + c/16) + (m - 16 s), whose rounding is 2^-20 of s), a conversion rounds two of them to bf16, the type of the matrix
-// operands.  Values are shared by all rows of a workgroup, so the wider one (eight waves, 256 rows) pays half as much a row.
+// Bound by the matrix cores, as attention over bf16 is: tiles of 64 tokens in LDS, and instruction streams over them (pasa_cache_pipes.hpp).
+// What differs is how a tile gets there: a thread holds one token's codes of a quarter of its channels, K or V, converts them and writes them
+// to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, so the wider one
+// (eight waves, 256 rows) pays half as much a row.
+//
+//   V: bf16(s c + m).  A shift and an and-or put two codes into fp16 numbers 1 + c/16, a mixed fma makes s c + m of each
+//     (16 s (1 + c/16) + (m - 16 s): the rounding of that is 2^-20 of s), a conversion rounds two of them to bf16: 2.5 instructions a value.
+//   K: fp16 s (c - 8), which is exact (s has 8 bits, c - 8 at most 3 or is a power of two), one packed fma for two codes: 1.5 instructions a
+//     value.  What that leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix instruction per 32 keys, with both factors as sums
+//     of two fp16 numbers (22 bits).  So the logits are those of the cache's values to binary32; with keys rounded to bf16 they are not,
+//     and lse is off by 1e-5.  Queries are fp16 times a power of two per row, which the row's logit scale takes back.
+//     Keys beyond +-16384 do not exist in a cache (pasa_cache_write), so 24 s is an fp16 number.
 #include "pasa_cache.hpp"
+#include "pasa_cache_pipes.hpp"
 #include "pasa_mfma_pipes.hpp"
 
 #include <type_traits>
@@ -31,6 +38,16 @@ PASA_DEVICE uint4 values8(uint32_t x, float a, float b) {
   }
   const bf16x2 r[4] = {{(__bf16)lo[0], (__bf16)lo[1]}, {(__bf16)lo[2], (__bf16)lo[3]}, {(__bf16)hi[0], (__bf16)hi[1]}, {(__bf16)hi[2], (__bf16)hi[3]}};
   return make_uint4(__builtin_bit_cast(uint32_t, r[0]), __builtin_bit_cast(uint32_t, r[1]), __builtin_bit_cast(uint32_t, r[2]), __builtin_bit_cast(uint32_t, r[3]));
+}
+
+// 8 keys' values s (c - 8) of a word of codes in fp16, in the order 0 4 1 5 2 6 3 7; a = 16 s, b = -24 s (twice each)
+PASA_DEVICE uint4 keys8(uint32_t x, f16x2 a, f16x2 b) {
+  const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 2) & 0x03c003c0u) | 0x3c003c00u,
+                         ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, h[i]), a, b));
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 template <int N>
@@ -68,19 +85,32 @@ struct TokenPart {
   // Row `token` of the tile at `tile`.  Not every row of the workgroup sees every token of it (whole == false): weights of zero do not
   // hide values that are not finite, so those leave V as zeros and make the token's keys NaN instead, which the rows that do not see
   // it replace.  (A row that does see it is NaN throughout then, not only in the channels of that group.)  there: some row sees the token
-  PASA_DEVICE void store(char* tile, int token, int quarter, bool whole, bool there) const {
+  // bias: the token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with (hi, lo, hi, 0) of
+  // the group's sum of q
+  PASA_DEVICE void store(char* tile, char* bias, int token, int quarter, bool whole, bool there) const {
     if constexpr (KEY) {
       bool poison = false;
       if (!whole) {
 #pragma unroll
         for (int g = 0; g < NP; ++g) poison |= !finite_param(v_par[g]);
       }
+      f16x2 a[NP], b[NP];
+      float mid = 0.f;
 #pragma unroll
-      for (int j = 0; j < NW; ++j) {
-        const uint32_t w = poison ? 0x7fc07fc0u : par[j * 32 / G];
-        const float s = bf16_low(w), a = 16.f * s;
-        *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, 4 * j + quarter)) = values8(code[j], a, bf16_high(w) - a);
+      for (int g = 0; g < NP; ++g) {
+        const uint32_t w = poison ? 0x7fc07fc0u : par[g];
+        const float s = bf16_low(w);
+        const _Float16 a1 = (_Float16)(16.f * s), b1 = (_Float16)(-24.f * s);
+        a[g] = f16x2{a1, a1};
+        b[g] = f16x2{b1, b1};
+        if (quarter == g) mid = fmaf(8.f, s, bf16_high(w));
       }
+      const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
+      const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
+      *reinterpret_cast<uint2*>(bias + token * 32 + quarter * 8) = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+#pragma unroll
+      for (int j = 0; j < NW; ++j)
+        *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, 4 * j + quarter)) = keys8(code[j], a[j * 32 / G], b[j * 32 / G]);
     } else {
       const uint32_t w = whole || (there && finite_param(par[0])) ? par[0] : 0u;
       const float s = bf16_low(w), a = 16.f * s, b = bf16_high(w) - a;
@@ -94,7 +124,8 @@ template <int D, int G, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnParams p) {
   constexpr int ROWS = WAVES * 32, TILE = 64 * 2 * D;
   constexpr bool BOTH = WAVES == 4;  // a thread has K and V of its token part; with eight waves four of them have K, four V
-  __shared__ __attribute__((aligned(1024))) char ring[4 * TILE];  // K, V of one tile, K, V of the next
+  constexpr int BIAS = 64 * 32;
+  __shared__ __attribute__((aligned(1024))) char ring[4 * TILE + 2 * BIAS];  // K, V of one tile, K, V of the next; offset operands of either
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
 
   // the last rows first: with a causal mask they have the most to do
@@ -121,16 +152,57 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   const int own = min(row, last_row), i_own = own / share, h_own = hkv * share + own % share;
   const int64_t row_off = b * p.stride_b + h_own * p.stride_h + i_own * p.stride_n;
   const int limit = limit_of(own);
-  bf16x8 qf[D / 16];
+  // q / 2^e in fp16, 2^e the power of two at the row's largest magnitude, in the order of a word's codes; qb: the groups' sums of that
+  f16x8 qf[D / 16], qb;
+  float c_row;  // logit scale times log2(e) times 2^e
+  {
+    uint4 raw[D / 16];
+    uint32_t top = 0u;
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p.q + row_off + 16 * s + 8 * h));
+    for (int s = 0; s < D / 16; ++s) {
+      raw[s] = *reinterpret_cast<const uint4*>(p.q + row_off + 16 * s + 8 * h);
+      const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
+    }
+    const u32x2 both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    const uint32_t e = min(max(max(both[0], both[1]) >> 23, 1u), 253u);
+    const float down = __uint_as_float((254u - e) << 23);
+    c_row = p.scale * __uint_as_float(e << 23);
+    float sum[D / G];
+#pragma unroll
+    for (int g = 0; g < D / G; ++g) sum[g] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = (i & 1 ? bf16_high(w[i / 2]) : bf16_low(w[i / 2])) * down;
+        const _Float16 y = (_Float16)x;
+        qf[s][i < 4 ? 2 * i : 2 * i - 7] = y;
+        sum[s * 16 / G] += (float)y;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {  // quarters 2 h and 2 h + 1
+      float t = 0.f;
+#pragma unroll
+      for (int g = 0; g < D / G; ++g) {
+        const float all = half_swap_sum(sum[g]);
+        if (2 * h + i == g) t = all;
+      }
+      const _Float16 hi = (_Float16)t, lo = (_Float16)(t - (float)hi);
+      qb[4 * i] = hi; qb[4 * i + 1] = lo; qb[4 * i + 2] = hi; qb[4 * i + 3] = (_Float16)0.f;
+    }
+  }
   f32x16 o[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) o[t] = f32x16{0};
   float m = -INFINITY, l = 0.f;
 
   const uint32_t ring_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
-  uint32_t k_read = ring_base + (uint32_t)lds_chunk_off<D>(ql, h), v_read[2];
+  const uint32_t k_read = ring_base + (uint32_t)lds_chunk_off<D>(ql, h), b_read = ring_base + (uint32_t)(4 * TILE + ql * 32 + h * 16);
+  uint32_t v_read[2];
   {
     const int i = lane & 15, r = 4 * h + (i >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (i & 3);
     v_read[0] = ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r, c >> 3) + (c & 7) * 2);
@@ -165,17 +237,22 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   };
   auto store = [&](int pair, bool whole) {
     char* const at = ring + pair * 2 * TILE;
-    if (has_k) kt.store(at, token, quarter, whole, in_page);
-    if (has_v) vt.store(at + TILE, token, quarter, whole, in_page);
+    if (has_k) kt.store(at, ring + 4 * TILE + pair * BIAS, token, quarter, whole, in_page);
+    if (has_v) vt.store(at + TILE, nullptr, token, quarter, whole, in_page);
   };
 
   // ---- one tile ----
-  auto compute = [&](int tile, int pair, bool whole) {
-    const uint32_t off = (uint32_t)(pair * 2 * TILE);
+  auto compute = [&](int tile, int pair, auto is_whole_tile) {
+    const uint32_t off = (uint32_t)(pair * 2 * TILE), k_at = k_read + off, b_at = b_read + (uint32_t)(pair * BIAS);
+    if constexpr (decltype(is_whole_tile)::value) {
+      cache_pipes::tile_step(k_at, b_at, v_read[0] + off, v_read[1] + off, qf, qb, o, m, l, c_row);
+      return;
+    }
+    // not every row sees every token
     f32x16 s0, s1;
     bf16x8 pf[4];
-    pipes::rows_x_q(k_read + off, qf, s0, s1);
-    if (!whole) {
+    cache_pipes::logits(k_at, b_at, qf, qb, s0, s1);
+    {
       const int rel = limit - 64 * tile - 4 * h;
       const uint32_t bits = followed(tile);
       int lim[4];
@@ -191,7 +268,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     float mx = fmaxf(s0[0], s1[0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, s0[r]), s1[r]);
-    mx = half_swap_max(mx) * p.scale;
+    mx = half_swap_max(mx) * c_row;
     if (__builtin_amdgcn_ballot_w64(mx > m)) {
       const float m_new = fmaxf(m, mx);
       const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -206,8 +283,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     float sum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s0[r] = __builtin_amdgcn_exp2f(fmaf(s0[r], p.scale, neg));
-      s1[r] = __builtin_amdgcn_exp2f(fmaf(s1[r], p.scale, neg));
+      s0[r] = __builtin_amdgcn_exp2f(fmaf(s0[r], c_row, neg));
+      s1[r] = __builtin_amdgcn_exp2f(fmaf(s1[r], c_row, neg));
       sum += s0[r] + s1[r];
     }
     l += sum;
@@ -227,24 +304,29 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     store(0, whole);
     if (t_begin + 1 < t_end) load(t_begin + 1, next_whole);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    for (int tile = t_begin; tile < t_end; ++tile) {
-      const int pair = (tile - t_begin) & 1;
+    // Half of the waves convert the next tile before their matrix work, half of them after it: a SIMD has one of either
+    const bool early = (wave & 4) == 0;
+    int tile = t_begin, pair = 0;
+    auto step = [&](auto is_whole_tile) {
       const bool more = tile + 1 < t_end, more2 = tile + 2 < t_end;
       const bool after_whole = more2 && is_whole(tile + 2);
-      // Half of the waves convert the next tile before their matrix work, half of them after it: a SIMD has one of either
-      const bool first = (wave & 4) == 0;
-      if (first && more) {
+      auto advance = [&]() {
         store(pair ^ 1, next_whole);
         if (more2) load(tile + 2, after_whole);
-      }
-      if (busy) compute(tile, pair, whole);
-      if (!first && more) {
-        store(pair ^ 1, next_whole);
-        if (more2) load(tile + 2, after_whole);
-      }
+      };
+      if (early && more) advance();
+      if (busy) compute(tile, pair, is_whole_tile);
+      if (!early && more) advance();
       whole = next_whole;
       next_whole = after_whole;
+      ++tile;
+      pair ^= 1;
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    while (tile < t_end) {
+#pragma unroll 1
+      while (tile < t_end && whole) step(std::true_type{});
+      if (tile < t_end) step(std::false_type{});
     }
   }
 

@@ -10,10 +10,13 @@ def token_bytes(d, group):
     return d + 8 * (d // group)
 
 
-def quantise(x, group):
-    """x bf16 [..., d] -> codes (int64, as x), scale, minimum (fp32 values that are bf16, [..., groups])"""
+MOST_KEY = 16384.0
+
+
+def quantise(x, group, most=math.inf):
+    """x bf16 [..., d], values up to most -> codes (int64, as x), scale, minimum (fp32 values that are bf16, [..., groups])"""
     g = x.double().reshape(*x.shape[:-1], -1, group)
-    bad = ~torch.isfinite(g).all(-1)
+    bad = ~(torch.isfinite(g) & (g.abs() <= most)).all(-1)
     g = torch.where(bad[..., None], torch.zeros_like(g), g)
     low, high = g.amin(-1), g.amax(-1)
     s = ((high - low) / 15).float().bfloat16().float()
@@ -68,7 +71,7 @@ class Model:
                 for h in range(self.H_kv):
                     run = self.run(pg, h)
                     for is_key, x in ((True, k), (False, v)):
-                        c, s, m = quantise(x[b, h, i], self.group)
+                        c, s, m = quantise(x[b, h, i], self.group, MOST_KEY if is_key else math.inf)
                         byte, shift = self.code_place(is_key)
                         code = torch.zeros(d // 2, dtype=torch.long).index_add_(0, byte, c.cpu() << shift)
                         at = (0 if is_key else page * d // 2) + slot * (d // 2)

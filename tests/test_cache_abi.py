@@ -138,3 +138,15 @@ def test_the_binding_refuses_what_the_library_cannot_see(P):
     refused("length", length=length.float())
     refused("length", length=torch.zeros(2, dtype=torch.int32))
     refused("n_new", n_new=torch.zeros(2, dtype=torch.int32))
+
+
+def test_generated_sequences_are_up_to_date():
+    """pasa_cache_pipes.hpp is written by gen_cache_pipes.py; the committed header must be what the generator emits"""
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc = os.path.join(root, "paper_2604_12219_amd", "csrc")
+    got = subprocess.run([sys.executable, "-c", "import gen_cache_pipes; print(gen_cache_pipes.gen(), end='')"], cwd=csrc, capture_output=True,
+                         text=True, check=True).stdout
+    with open(os.path.join(csrc, "pasa_cache_pipes.hpp")) as f:
+        assert f.read() == got
