@@ -215,22 +215,31 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   TokenPart<D, G, true> kt;
   TokenPart<D, G, false> vt;
   bool in_page = false;  // of the token part that is loaded: its page is followed
+  auto is_page = [&](int pg) -> bool { return pg >= 0 && pg < p.c.n_pages; };
+  // Whether all pages of the workgroup's tokens are followed (or else every tile is masked: `followed` below looks each of them up)
+  bool pages_good = true;
+  {
+    const int first = t_begin * 64 >> p.c.log_page, last = (min(64 * t_end, seq.length) - 1) >> p.c.log_page;
+    for (int j = first + tid; j <= last; j += WAVES * 64) pages_good &= is_page(p.c.pages[(int64_t)b * p.c.max_pages + j]);
+    pages_good = __syncthreads_and(pages_good);
+  }
   auto followed = [&](int tile) -> uint32_t {  // bit t: the page of tokens 64 tile + 16 t .. is followed
     uint32_t bits = 0u;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int pg = table[min(64 * tile + 16 * t, seq.length - 1) >> p.c.log_page];
-      bits |= (uint32_t)(pg >= 0 && pg < p.c.n_pages) << t;
-    }
+    for (int t = 0; t < 4; ++t) bits |= (uint32_t)is_page(table[min(64 * tile + 16 * t, seq.length - 1) >> p.c.log_page]) << t;
     return bits;
   };
-  auto is_whole = [&](int tile) -> bool { return 64 * tile + 64 <= limit_all && followed(tile) == 15u; };
-  auto load = [&](int tile, bool whole) {
+  auto is_whole = [&](int tile) -> bool { return pages_good && 64 * tile + 64 <= limit_all; };
+  // A token's page is looked up a step before its codes are requested, these a step before they are converted
+  const int64_t pool_page = (int64_t)p.c.H_kv * p.c.head_bytes;
+  const uint8_t* const pool_head = p.c.pool + (int64_t)hkv * p.c.head_bytes;
+  int page_next = 0;
+  auto look_up = [&](int tile) { page_next = p.c.pages[(int64_t)b * p.c.max_pages + (min(64 * tile + token, seq.length - 1) >> p.c.log_page)]; };
+  auto load = [&](int tile, bool whole) {  // after look_up(tile)
     const int pos = 64 * tile + token;
-    const int pg = p.c.pages[(int64_t)b * p.c.max_pages + (min(pos, seq.length - 1) >> p.c.log_page)];
-    const bool ok = pg >= 0 && pg < p.c.n_pages;
+    const bool ok = is_page(page_next);
     in_page = ok && pos < limit_any;
-    const uint8_t* const run = p.c.pool + ((int64_t)(ok ? pg : 0) * p.c.H_kv + hkv) * p.c.head_bytes;
+    const uint8_t* const run = pool_head + (ok ? page_next : 0) * pool_page;
     const uint32_t slot = (uint32_t)pos & (page - 1u);
     if (has_k) kt.load(run, page, slot, quarter, whole);
     if (has_v) vt.load(run, page, slot, quarter, whole);
@@ -299,20 +308,23 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   };
 
   if (t_begin < t_end) {
-    bool whole = is_whole(t_begin), next_whole = t_begin + 1 < t_end && is_whole(t_begin + 1);
+    bool whole = is_whole(t_begin), next_whole = is_whole(t_begin + 1);
+    look_up(t_begin);
     load(t_begin, whole);
+    look_up(t_begin + 1);
     store(0, whole);
-    if (t_begin + 1 < t_end) load(t_begin + 1, next_whole);
+    load(t_begin + 1, next_whole);
+    look_up(t_begin + 2);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     // Half of the waves convert the next tile before their matrix work, half of them after it: a SIMD has one of either
     const bool early = (wave & 4) == 0;
     int tile = t_begin, pair = 0;
     auto step = [&](auto is_whole_tile) {
-      const bool more = tile + 1 < t_end, more2 = tile + 2 < t_end;
-      const bool after_whole = more2 && is_whole(tile + 2);
+      const bool more = tile + 1 < t_end, after_whole = is_whole(tile + 2);
       auto advance = [&]() {
         store(pair ^ 1, next_whole);
-        if (more2) load(tile + 2, after_whole);
+        load(tile + 2, after_whole);  // (behind the last tile: some token of the sequence, not used)
+        look_up(tile + 3);
       };
       if (early && more) advance();
       if (busy) compute(tile, pair, is_whole_tile);
