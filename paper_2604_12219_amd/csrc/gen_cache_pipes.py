@@ -10,88 +10,140 @@ Run `python gen_cache_pipes.py` in this directory after changing it; the header 
 import os
 
 import gen_mfma_pipes as base
-from gen_mfma_pipes import F, FS_O, FS_P0, FS_P1, FS_S0, FS_S1, FS_T, MFMA, NOP_AFTER, off, vr
+from gen_mfma_pipes import FS_P0, FS_P1, FS_S0, FS_S1, FS_T, MFMA, NOP_AFTER, Cold, F, exp_stream, growth, max_stream, off, pending, pour, vr
 
 MFMA_F16 = "v_mfma_f32_32x32x16_f16"
 BIAS_ROW = 32  # bytes of a key's offset operands
 
 
-class Pipe(base.LdsPipe):
-    def issue(self, k, load):
-        if load[0] == "b":  # offset operands of 32 keys
-            self.lines.append(f"ds_read_b128 {F(k % self.nbuf)}, %[ab]{off(load[2] * 32 * BIAS_ROW)}")
-            self.issued.append(1)
-        else:
-            super().issue(k, load)
-
-
-def logits(D, half):
+def qk(D, half):
     acc = vr(FS_S0 if half == 0 else FS_S1, 16)
     return [dict(op=MFMA_F16, acc=acc, first=True, b="%[qb]", load=("b", 0, half))] + \
         [dict(op=MFMA_F16, acc=acc, first=False, b=f"%[q{st}]", load=("k", st, half)) for st in range(D // 16)]
 
 
-def run(D, mf, before, after):
-    lines = []
-    pipe = Pipe(lines, D)
-    pipe.k_addresses()
+def pv(D, half):
+    return [dict(op=MFMA, **m) for m in base.pv_mfmas(D, half)]
+
+
+def run(D, mf, before, after, k_slot, v_slot, prologue=()):
+    """MFMA k of `mf` with its operand fetch issued six MFMAs ahead (as pipe_run of gen_mfma_pipes.py); k_slot, v_slot: which of the two
+    K and V tiles of the ring"""
+    lines, issued, nbuf = [], [], 6
+    k_off, b_off, v_off = k_slot * 256 * D, k_slot * 64 * BIAS_ROW, v_slot * 256 * D
+
+    def issue(k):
+        f = k % nbuf
+        kind, a, b = mf[k]["load"]
+        if kind == "b":  # offset operands of 32 keys
+            lines.append(f"ds_read_b128 {F(f)}, %[ab]{off(b_off + b * 32 * BIAS_ROW)}")
+        elif kind == "k":
+            lines.append(f"ds_read_b128 {F(f)}, %[ka{a}]{off(k_off + b * 64 * D)}")
+        else:
+            lines.append(f"ds_read_b64_tr_b16 {base.Flo(f)}, %[va{2 * b}]{off(v_off + a * 32 * D)}")
+            lines.append(f"ds_read_b64_tr_b16 {base.Fhi(f)}, %[va{2 * b + 1}]{off(v_off + a * 32 * D)}")
+        issued.append(2 if kind == "v" else 1)
+
     n = len(mf)
-    for k in range(min(pipe.nbuf, n)):
-        pipe.issue(k, mf[k]["load"])
+    for k in range(min(nbuf, n)):
+        issue(k)
+    lines += list(prologue)
     for k in range(n):
-        pipe.wait_for(k)
+        outstanding = sum(issued[k + 1:])
+        assert outstanding <= 15
+        lines.append(f"s_waitcnt lgkmcnt({outstanding})")
         lines += before.get(k, [])
         m = mf[k]
-        lines.append(f"{m['op']} {m['acc']}, {F(k % pipe.nbuf)}, {m['b']}, {'0' if m['first'] else m['acc']}")
-        if k + pipe.nbuf < n:
-            pipe.issue(k + pipe.nbuf, mf[k + pipe.nbuf]["load"])
+        lines.append(f"{m['op']} {m['acc']}, {F(k % nbuf)}, {m['b']}, {'0' if m['first'] else m['acc']}")
+        if k + nbuf < n:
+            issue(k + nbuf)
         lines += after.get(k, [])
-    return lines + [NOP_AFTER]
+    return lines
 
 
-def tile_step(D):
-    """logits, online softmax and P V of one 64-key tile (fused_step of gen_mfma_pipes.py)"""
-    nl, nt = D // 16 + 1, D // 32
-    n_o = 16 * nt
-    mf = logits(D, 0) + logits(D, 1)
-    for half in range(2):
-        for ks in range(2):
-            for t in range(nt):
-                mf.append(dict(op=MFMA, acc=vr(FS_O + 16 * t, 16), first=False, b=vr((FS_P0 if half == 0 else FS_P1) + 4 * ks, 4),
-                               load=("v", 2 * half + ks, t)))
+def pipe_step(D, par):
+    """P V of the tile in V slot par, logits of the next one, in the other K slot"""
+    n_o = 16 * (D // 32)
+    mf = qk(D, 0) + pv(D, 0) + qk(D, 1) + pv(D, 1)
+    n = len(mf)
+    cold = Cold(f"ps{par}_")
+    corr1 = vr(FS_T + 3)
     after = {}
-    pv0_end = 2 * nl + 2 * nt - 1
-    base.spread(after, nl + 1, 2 * nl - 1, base.max_stream(FS_S0) + base.raise_max(n_o, True) + base.exp_stream(FS_S0, FS_P0))
-    base.spread(after, 2 * nl + 1, pv0_end, base.max_stream(FS_S1) + base.raise_max(n_o, False) + base.exp_stream(FS_S1, FS_P1))
-    after[pv0_end] += ["s_cmp_eq_u64 %[flag], 0", "s_cbranch_scc1 .Lfs_nors_%=", "s_nop 13"] + \
-        [f"v_mul_f32 {vr(FS_O + i)}, {vr(FS_O + i)}, {vr(FS_T + 3)}" for i in range(n_o)] + [".Lfs_nors_%=:"]
-    before = {2 * nl: ["s_nop 1"], 2 * nl + 2 * nt: ["s_nop 1"]}  # P^T / accumulators were written by VALU just before
-    return run(D, mf, before, after)
+    after[1] = list(pending(cold, "%[flag]", "%[corr]", n_o, "s_nop 3"))  # left by the step before
+    # (done with S1 before the MFMAs of the second half write it; S0 is long complete)
+    pour(after, n, [growth(cold, "%[flag1]", corr1)] + exp_stream(FS_S1, FS_P1), first=1, end=0.5)
+    pour(after, n, max_stream(FS_S0) + [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S0, FS_P0), begin=0.5)
+    k = n // 2 + 1  # the P V of the first half is through
+    after[k] = list(pending(cold, "%[flag1]", corr1, n_o, "s_nop 3")) + after.get(k, [])
+    return run(D, mf, {}, after, 1 - par, par, prologue=max_stream(FS_S1)) + cold.text()
+
+
+def pipe_start(D, par):
+    """logits of the tile in K slot par and the softmax of its first half"""
+    mf = qk(D, 0) + qk(D, 1)
+    n, q = len(mf), len(mf) // 2
+    cold = Cold(f"pb{par}_")
+    after = {}
+    pour(after, n, max_stream(FS_S0) + [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S0, FS_P0), first=q + 1, begin=(q + 1) / n)
+    return run(D, mf, {}, after, par, 0) + [NOP_AFTER] + cold.text()
+
+
+def pipe_end(D, par):
+    """P V of the last tile (V slot par) and the softmax of its second half"""
+    n_o = 16 * (D // 32)
+    mf = pv(D, 0) + pv(D, 1)
+    q = len(mf) // 2
+    cold = Cold(f"pe{par}_")
+    after = {}
+    pour(after, q, [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S1, FS_P1))
+    before = {q: list(pending(cold, "%[flag]", "%[corr]", n_o, NOP_AFTER)) + ["s_nop 1"]}
+    return run(D, mf, before, after, 0, par, prologue=list(pending(cold, "%[flag]", "%[corr]", n_o, NOP_AFTER)) + max_stream(FS_S1) + ["s_nop 1"]) + \
+        [NOP_AFTER] + cold.text()
 
 
 def gen():
     out = ["// GENERATED by gen_cache_pipes.py -- do not edit.  LDS-read + MFMA sequences of attention over the 4-bit cache (gfx950), one asm\n"
-           "// statement each; v168..v255 are theirs.\n"
-           "#pragma once\n#include \"pasa_device.hpp\"\n\ntypedef _Float16 f16x8 __attribute__((ext_vector_type(8)));\n\nnamespace cache_pipes {\n\n"]
+           "// statement each.\n"
+           "#pragma once\n#include \"pasa_mfma_pipes.hpp\"\n\ntypedef _Float16 f16x8 __attribute__((ext_vector_type(8)));\n\nnamespace cache_pipes {\n\n"
+           "using pipes::PipeState;\n\n"]
+    s0, p1, rest = range(FS_S0, FS_S0 + 16), range(FS_P1, FS_P1 + 8), list(range(FS_T, 256))
     for D in (128, 64):
         ns, nt = D // 16, D // 32
-        qin = [f'[q{s}] "v"(q[{s}])' for s in range(ns)] + ['[qb] "v"(qb)']
-        text = lambda lines: "\n".join(f'      "{l}\\n\\t"' for l in lines)
-        clob = lambda regs, more: ", ".join([f'"v{r}"' for r in regs] + [f'"{c}"' for c in more])
-        s_out = '"=&{v[168:183]}"(c0), "=&{v[184:199]}"(c1)'
-        s_in = ", ".join(['[ak] "v"(ak)', '[ab] "v"(ab)'] + qin)
-        out.append(f"// c0, c1 = logits of the tile's keys 0..31 and 32..63;  ak: K tile address + lane's row-fragment offset, ab: the same of its offset operands\n"
-                   f"PASA_DEVICE void logits(uint32_t ak, uint32_t ab, const f16x8 (&q)[{ns}], f16x8 qb, f32x16& c0, f32x16& c1) {{\n"
-                   f"  asm volatile(\n{text(run(D, logits(D, 0) + logits(D, 1), {}, {}))}\n      : {s_out}\n      : {s_in}\n"
-                   f"      : {clob(range(200, 256), ['memory'])});\n}}\n\n")
-        outs = base.o_ops(nt) + ['[m] "+v"(m)', '[l] "+v"(l)', '[flag] "=&s"(flag)']
-        ins = ['[ak] "v"(ak)', '[ab] "v"(ab)', '[av0] "v"(av0)', '[av1] "v"(av1)', '[c] "v"(c)'] + qin
-        out.append(f"// One whole 64-key tile against the wave's 32 queries: logits, online softmax, P V.  av0, av1: V tile address + the two column-fragment\n"
-                   f"// offsets; m, l: running maximum (log2 units) and normaliser share; c: the lane's logit scale * log2(e)\n"
-                   f"PASA_DEVICE void tile_step(uint32_t ak, uint32_t ab, uint32_t av0, uint32_t av1, const f16x8 (&q)[{ns}], f16x8 qb, f32x16 (&o)[{nt}], float& m,\n"
-                   f"                           float& l, float c) {{\n  uint64_t flag;\n"
-                   f"  asm volatile(\n{text(tile_step(D))}\n      : {', '.join(outs)}\n      : {', '.join(ins)}\n"
-                   f"      : {clob(range(base.FUSED_CLOBBER_LO, 256), ['memory', 'scc', 'vcc'])});\n}}\n\n")
+
+        def emit(comment, head, pre, lines, outs, ins, clob):
+            text = "\n".join(f'      "{l}\\n\\t"' for l in lines)
+            regs = ", ".join([f'"v{r}"' for r in clob] + ['"memory"', '"scc"', '"vcc"'])
+            out.append(f"{comment}PASA_DEVICE void {head} {{\n{pre}  asm volatile(\n{text}\n      : {', '.join(outs)}\n      : {', '.join(ins)}\n"
+                       f"      : {regs});\n}}\n\n")
+
+        q_args = f"const f16x8 (&q)[{ns}], f16x8 qb"
+        state = f"f32x16 (&o)[{nt}], float& m, float& l, PipeState& st"
+        ml = ['[m] "+v"(m)', '[l] "+v"(l)']
+        sb = '"+{v[184:199]}"(st.s1)'
+        pa = [f'"+{{v[{200 + 4 * k}:{203 + 4 * k}]}}"(st.p0[{k}])' for k in range(2)]
+        carry = ['[corr] "+v"(st.corr)', '[flag] "+s"(st.flag)']
+        kin = [f'[ka{s}] "v"(ka[{s}])' for s in range(ns)] + ['[ab] "v"(ab)'] + [f'[q{s}] "v"(q[{s}])' for s in range(ns)] + ['[qb] "v"(qb)']
+        vin = [f'[va{s}] "v"(va[{s}])' for s in range(2 * nt)]
+        cin, par_in = ['[c] "v"(c)'], ['[par] "s"(par)']
+        k_args = f"const uint32_t (&ka)[{ns}], uint32_t ab"
+        emit("// c0, c1 = logits of keys 0..31 and 32..63 of the tile in K slot par.  ka, ab: the lane's addresses of the row fragments and of the offset\n"
+             "// operands in K slot 0; q, qb: the queries and what they multiply the offsets with\n",
+             f"logits(int par, {k_args}, {q_args}, f32x16& c0, f32x16& c1)", "",
+             base.both_parities("lg", lambda par: run(D, qk(D, 0) + qk(D, 1), {}, {}, par, 0) + [NOP_AFTER]),
+             ['"=&{v[168:183]}"(c0)', '"=&{v[184:199]}"(c1)'], kin + par_in, range(226, 256))
+        emit("// Start of a run of pipelined steps: logits of the tile in K slot par, softmax of its first half.  c: the lane's logit scale * log2(e);\n"
+             "// corr, flag of the state are outputs\n",
+             f"pipe_start(int par, {k_args}, {q_args}, float& m, float& l, float c, PipeState& st)", "",
+             base.both_parities("pb", lambda par: pipe_start(D, par)),
+             ml + ['"=&{v[184:199]}"(st.s1)'] + [x.replace("+", "=&") for x in pa] + ['[corr] "=&v"(st.corr)', '[flag] "=&s"(st.flag)'],
+             kin + cin + par_in, list(s0) + list(p1) + rest)
+        emit("// P V of the tile in V slot par, logits of the next one, in the other K slot.  va: the lane's addresses of the column fragments in V slot 0\n",
+             f"pipe_step(int par, {k_args}, const uint32_t (&va)[{2 * nt}], {q_args}, {state}, float c)", "  uint64_t flag1;\n",
+             base.both_parities("ps", lambda par: pipe_step(D, par)),
+             base.o_ops(nt) + ml + [sb] + pa + carry + ['[flag1] "=&s"(flag1)'], kin + vin + cin + par_in, list(s0) + list(p1) + rest)
+        emit("// End of a run: P V of the tile in V slot par\n",
+             f"pipe_end(int par, const uint32_t (&va)[{2 * nt}], {state}, float c)", "", base.both_parities("pe", lambda par: pipe_end(D, par)),
+             base.o_ops(nt) + ml + [sb] + pa + carry, vin + cin + par_in, list(s0) + list(p1) + rest)
     out.append("}  // namespace cache_pipes\n")
     return "".join(out)
 

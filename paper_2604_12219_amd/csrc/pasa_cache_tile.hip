@@ -1,7 +1,7 @@
 // Attention of many new rows over the 4-bit cache: the matrix-core side of pasa_cache_attn.hip.
 //
 // Bound by the matrix cores, as attention over bf16 is: tiles of 64 tokens in LDS, and instruction streams over them (pasa_cache_pipes.hpp).
-// What differs is how a tile gets there: a thread holds one token's codes of a quarter of its channels, K or V, converts them and writes them
+// What differs is how a tile gets there: a thread holds a few code words of one token, of K and of V, converts them and writes them
 // to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, so the wider one
 // (eight waves, 256 rows) pays half as much a row.
 //
@@ -14,9 +14,6 @@
 //     Keys beyond +-16384 do not exist in a cache (pasa_cache_write), so 24 s is an fp16 number.
 #include "pasa_cache.hpp"
 #include "pasa_cache_pipes.hpp"
-#include "pasa_mfma_pipes.hpp"
-
-#include <type_traits>
 
 namespace {
 
@@ -66,65 +63,79 @@ PASA_DEVICE void load_words(const uint8_t* at, uint32_t (&w)[N]) {
 
 PASA_DEVICE bool finite_param(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
 
-// One token's share of a tile: a quarter of its K (or V) codes, and the parameters that they need
-template <int D, int G, bool KEY>
-struct TokenPart {
+// A thread's share of a tile: N code words of one token's K, and as many of its V, with the parameters they need.
+// `part` counts the threads of a token: they divide each quarter (the words of one q) of the K codes, and the V codes in order.
+template <int D, int G, int N>
+struct Share {
   typedef CacheLayout<D, G> L;
-  static constexpr int NW = D / 32, NP = KEY ? D / G : 1;
-  uint32_t code[NW], par[NP];
-  uint32_t v_par[KEY ? D / G : 1];  // K of a tile that not every row sees whole: the token's V parameters
-  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, int quarter, bool whole) {
-    load_words<NW>(run + (KEY ? L::k_codes(page) : L::v_codes(page)) + slot * L::CODE + quarter * (L::CODE / 4), code);
-    if constexpr (KEY) {
-      load_words<NP>(run + L::k_params(page) + slot * L::PARAM, par);
-      if (!whole) load_words<NP>(run + L::v_params(page) + slot * L::PARAM, v_par);
-    } else {
-      load_words<1>(run + L::v_params(page) + slot * L::PARAM + 4 * (quarter * (D / 4) / G), par);
-    }
+  static constexpr int PARTS = D / 8 / N, PER_Q = D / 32 / N;  // threads of a token, of a quarter
+  static constexpr int KG = N * 32 > G ? N * 32 / G : 1;       // groups of a thread's K words
+  static __device__ constexpr int k_group(int j) { return j * 32 / G; }  // of the j-th word, among them
+  static PASA_DEVICE int quarter(int part) { return part / PER_Q; }
+  static PASA_DEVICE int first_word(int part) { return part % PER_Q * N; }  // in its quarter
+};
+template <int D, int G, int N>
+struct KeyShare : Share<D, G, N> {
+  typedef Share<D, G, N> S;
+  typedef typename S::L L;
+  uint32_t code[N], par[S::KG], bias;  // bias: the parameter of group `quarter`
+  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, int part) {
+    load_words<N>(run + L::k_codes(page) + slot * L::CODE + 4 * (S::quarter(part) * (D / 32) + S::first_word(part)), code);
+    const uint8_t* const at = run + L::k_params(page) + slot * L::PARAM;
+    load_words<S::KG>(at + 4 * (S::first_word(part) * 32 / G), par);
+    bias = *reinterpret_cast<const uint32_t*>(at + 4 * min(S::quarter(part), L::NG - 1));
   }
-  // Row `token` of the tile at `tile`.  Not every row of the workgroup sees every token of it (whole == false): weights of zero do not
-  // hide values that are not finite, so those leave V as zeros and make the token's keys NaN instead, which the rows that do not see
-  // it replace.  (A row that does see it is NaN throughout then, not only in the channels of that group.)  there: some row sees the token
-  // bias: the token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with (hi, lo, hi, 0) of
-  // the group's sum of q
-  PASA_DEVICE void store(char* tile, char* bias, int token, int quarter, bool whole, bool there) const {
-    if constexpr (KEY) {
-      bool poison = false;
-      if (!whole) {
-#pragma unroll
-        for (int g = 0; g < NP; ++g) poison |= !finite_param(v_par[g]);
-      }
-      f16x2 a[NP], b[NP];
-      float mid = 0.f;
-#pragma unroll
-      for (int g = 0; g < NP; ++g) {
-        const uint32_t w = poison ? 0x7fc07fc0u : par[g];
-        const float s = bf16_low(w);
-        const _Float16 a1 = (_Float16)(16.f * s), b1 = (_Float16)(-24.f * s);
-        a[g] = f16x2{a1, a1};
-        b[g] = f16x2{b1, b1};
-        if (quarter == g) mid = fmaf(8.f, s, bf16_high(w));
-      }
+  // Into row `token` of the tile at `tile`.
+  // at_bias: the token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with
+  // (hi, lo, hi, 0) of the group's sum of q
+  PASA_DEVICE void store(char* tile, char* at_bias, int token, int part) const {
+    const int quarter = S::quarter(part);
+    {
+      const float mid = fmaf(8.f, bf16_low(bias), bf16_high(bias));
       const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
       const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
-      *reinterpret_cast<uint2*>(bias + token * 32 + quarter * 8) = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
-#pragma unroll
-      for (int j = 0; j < NW; ++j)
-        *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, 4 * j + quarter)) = keys8(code[j], a[j * 32 / G], b[j * 32 / G]);
-    } else {
-      const uint32_t w = whole || (there && finite_param(par[0])) ? par[0] : 0u;
-      const float s = bf16_low(w), a = 16.f * s, b = bf16_high(w) - a;
-#pragma unroll
-      for (int j = 0; j < NW; ++j) *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, quarter * NW + j)) = values8(code[j], a, b);
+      uint2 x = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+      if (quarter >= L::NG) x = make_uint2(0u, 0u);
+      *reinterpret_cast<uint2*>(at_bias + token * 32 + quarter * 8) = x;
     }
+    f16x2 a[S::KG], b[S::KG];
+#pragma unroll
+    for (int g = 0; g < S::KG; ++g) {
+      const float s = bf16_low(par[g]);
+      const _Float16 a1 = (_Float16)(16.f * s), b1 = (_Float16)(-24.f * s);
+      a[g] = f16x2{a1, a1};
+      b[g] = f16x2{b1, b1};
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, 4 * (S::first_word(part) + j) + quarter)) = keys8(code[j], a[S::k_group(j)], b[S::k_group(j)]);
+  }
+};
+template <int D, int G, int N>
+struct ValueShare : Share<D, G, N> {
+  typedef Share<D, G, N> S;
+  typedef typename S::L L;
+  uint32_t code[N], par;
+  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, int part) {
+    load_words<N>(run + L::v_codes(page) + slot * L::CODE + 4 * N * part, code);
+    par = *reinterpret_cast<const uint32_t*>(run + L::v_params(page) + slot * L::PARAM + 4 * (8 * N * part / G));
+  }
+  PASA_DEVICE void store(char* tile, int token, int part, bool hide) const {
+    const uint32_t w = hide ? 0u : par;
+    const float s = bf16_low(w), a = 16.f * s, b = bf16_high(w) - a;
+#pragma unroll
+    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, N * part + j)) = values8(code[j], a, b);
   }
 };
 
 template <int D, int G, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnParams p) {
+  typedef CacheLayout<D, G> L;
   constexpr int ROWS = WAVES * 32, TILE = 64 * 2 * D;
-  constexpr bool BOTH = WAVES == 4;  // a thread has K and V of its token part; with eight waves four of them have K, four V
+  constexpr int N = D / WAVES / 8;  // code words of K, and of V, that a thread converts
+  typedef Share<D, G, N> S;
   constexpr int BIAS = 64 * 32;
+  __shared__ float bad[2][64];  // of a tile that not every row sees whole: NaN for a token that has values which are not finite, 0 for others
   __shared__ __attribute__((aligned(1024))) char ring[4 * TILE + 2 * BIAS];  // K, V of one tile, K, V of the next; offset operands of either
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
 
@@ -148,7 +159,6 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
 
   // this wave's rows, a lane's row in either half-wave
   const int row = row0 + wave * 32 + ql;
-  const bool busy = row0 + wave * 32 <= last_row;  // (wave-uniform)
   const int own = min(row, last_row), i_own = own / share, h_own = hkv * share + own % share;
   const int64_t row_off = b * p.stride_b + h_own * p.stride_h + i_own * p.stride_n;
   const int limit = limit_of(own);
@@ -201,20 +211,24 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   float m = -INFINITY, l = 0.f;
 
   const uint32_t ring_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
-  const uint32_t k_read = ring_base + (uint32_t)lds_chunk_off<D>(ql, h), b_read = ring_base + (uint32_t)(4 * TILE + ql * 32 + h * 16);
-  uint32_t v_read[2];
+  // the lane's addresses of the operand fetches in the first K and V slot
+  uint32_t ka[D / 16], va[2 * (D / 32)];
+  const uint32_t ab = ring_base + (uint32_t)(4 * TILE + ql * 32 + h * 16);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) ka[s] = (ring_base + (uint32_t)lds_chunk_off<D>(ql, h)) ^ (uint32_t)(s << 5);
   {
     const int i = lane & 15, r = 4 * h + (i >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (i & 3);
-    v_read[0] = ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r, c >> 3) + (c & 7) * 2);
-    v_read[1] = ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r + 8, c >> 3) + (c & 7) * 2);
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      va[2 * t] = (ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r, c >> 3) + (c & 7) * 2)) ^ (uint32_t)(t << 6);
+      va[2 * t + 1] = (ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r + 8, c >> 3) + (c & 7) * 2)) ^ (uint32_t)(t << 6);
+    }
   }
 
   // ---- how a tile gets into LDS ----
-  const int token = (tid & 255) >> 2, quarter = tid & 3;
-  const bool has_k = BOTH || wave < 4, has_v = BOTH || wave >= 4;
-  TokenPart<D, G, true> kt;
-  TokenPart<D, G, false> vt;
-  bool in_page = false;  // of the token part that is loaded: its page is followed
+  const int token = tid / S::PARTS, part = tid % S::PARTS;
+  KeyShare<D, G, N> kt;
+  ValueShare<D, G, N> vt;
   auto is_page = [&](int pg) -> bool { return pg >= 0 && pg < p.c.n_pages; };
   // Whether all pages of the workgroup's tokens are followed (or else every tile is masked: `followed` below looks each of them up)
   bool pages_good = true;
@@ -229,50 +243,58 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     for (int t = 0; t < 4; ++t) bits |= (uint32_t)is_page(table[min(64 * tile + 16 * t, seq.length - 1) >> p.c.log_page]) << t;
     return bits;
   };
-  auto is_whole = [&](int tile) -> bool { return pages_good && 64 * tile + 64 <= limit_all; };
-  // A token's page is looked up a step before its codes are requested, these a step before they are converted
+  const int t_whole = pages_good ? max(min(limit_all >> 6, t_end), t_begin) : t_begin;  // before it every row sees every token
+  // A token's page is looked up a step before its codes are requested, these a step before they are converted.  (Behind the last tile: some
+  // token of the sequence, converted and not used)
   const int64_t pool_page = (int64_t)p.c.H_kv * p.c.head_bytes;
   const uint8_t* const pool_head = p.c.pool + (int64_t)hkv * p.c.head_bytes;
-  int page_next = 0;
-  auto look_up = [&](int tile) { page_next = p.c.pages[(int64_t)b * p.c.max_pages + (min(64 * tile + token, seq.length - 1) >> p.c.log_page)]; };
-  auto load = [&](int tile, bool whole) {  // after look_up(tile)
-    const int pos = 64 * tile + token;
-    const bool ok = is_page(page_next);
-    in_page = ok && pos < limit_any;
-    const uint8_t* const run = pool_head + (ok ? page_next : 0) * pool_page;
-    const uint32_t slot = (uint32_t)pos & (page - 1u);
-    if (has_k) kt.load(run, page, slot, quarter, whole);
-    if (has_v) vt.load(run, page, slot, quarter, whole);
-  };
-  auto store = [&](int pair, bool whole) {
-    char* const at = ring + pair * 2 * TILE;
-    if (has_k) kt.store(at, ring + 4 * TILE + pair * BIAS, token, quarter, whole, in_page);
-    if (has_v) vt.store(at + TILE, nullptr, token, quarter, whole, in_page);
-  };
-
-  // ---- one tile ----
-  auto compute = [&](int tile, int pair, auto is_whole_tile) {
-    const uint32_t off = (uint32_t)(pair * 2 * TILE), k_at = k_read + off, b_at = b_read + (uint32_t)(pair * BIAS);
-    if constexpr (decltype(is_whole_tile)::value) {
-      cache_pipes::tile_step(k_at, b_at, v_read[0] + off, v_read[1] + off, qf, qb, o, m, l, c_row);
-      return;
+  auto look_up = [&](int tile) -> int { return p.c.pages[(int64_t)b * p.c.max_pages + (min(64 * tile + token, seq.length - 1) >> p.c.log_page)]; };
+  auto run_of = [&](int pg) -> const uint8_t* { return pool_head + (is_page(pg) ? pg : 0) * pool_page; };
+  auto slot_of = [&](int tile) -> uint32_t { return (uint32_t)(64 * tile + token) & (page - 1u); };
+  const uint8_t *k_run, *v_run;  // of the tiles to be requested next
+  int next_page;                 // of the tile after k_run's
+  auto store_k = [&](const KeyShare<D, G, N>& share, int par) { share.store(ring + par * 2 * TILE, ring + 4 * TILE + par * BIAS, token, part); };
+  // Weights of zero do not hide values that are not finite from the rows that do not see them: in a tile that is not whole such values
+  // become zeros, and `bad` says so to the rows that do see the token (which are NaN throughout then, not only in the channels of that group)
+  auto store_v = [&](int tile, int par) {
+    bool hide = false;
+    if (tile >= t_whole) {
+      const bool finite = finite_param(vt.par);
+      hide = !finite || 64 * tile + token >= limit_any || (!pages_good && !is_page(look_up(tile)));
+      const uint64_t not_finite = __builtin_amdgcn_ballot_w64(!finite) >> (lane & ~(S::PARTS - 1));
+      if (part == 0) bad[par][token] = (not_finite & ((1u << S::PARTS) - 1u)) ? NAN : 0.f;
     }
-    // not every row sees every token
+    vt.store(ring + par * 2 * TILE + TILE, token, part, hide);
+  };
+  // While tile t (in the slots par) is worked on: K of t + 2 and V of t + 1 into LDS
+  auto advance = [&](int t, int par) {
+    store_k(kt, par);
+    store_v(t + 1, par ^ 1);
+    kt.load(k_run, page, slot_of(t + 3), part);
+    vt.load(v_run, page, slot_of(t + 2), part);
+    v_run = k_run;
+    k_run = run_of(next_page);
+    next_page = look_up(t + 5);
+  };
+  auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  // ---- a tile of which not every row sees every token ----
+  auto masked_tile = [&](int tile, int par) {
     f32x16 s0, s1;
     bf16x8 pf[4];
-    cache_pipes::logits(k_at, b_at, qf, qb, s0, s1);
-    {
-      const int rel = limit - 64 * tile - 4 * h;
-      const uint32_t bits = followed(tile);
-      int lim[4];
+    cache_pipes::logits(par, ka, ab, qf, qb, s0, s1);
+    const int rel = limit - 64 * tile - 4 * h;
+    const uint32_t bits = followed(tile);
+    int lim[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) lim[t] = (bits >> t) & 1u ? rel : -64;
+    for (int t = 0; t < 4; ++t) lim[t] = (bits >> t) & 1u ? rel : -64;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = mfma_row(r, 0);
-        if (key >= lim[r >> 3]) s0[r] = -INFINITY;
-        if (key + 32 >= lim[2 + (r >> 3)]) s1[r] = -INFINITY;
-      }
+    for (int r = 0; r < 16; ++r) {
+      const int key = mfma_row(r, 0);
+      s0[r] += bad[par][key + 4 * h];
+      s1[r] += bad[par][key + 32 + 4 * h];
+      if (key >= lim[r >> 3]) s0[r] = -INFINITY;
+      if (key + 32 >= lim[2 + (r >> 3)]) s1[r] = -INFINITY;
     }
     float mx = fmaxf(s0[0], s1[0]);
 #pragma unroll
@@ -304,41 +326,57 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
       pf[2][i] = (__bf16)s1[i];
       pf[3][i] = (__bf16)s1[8 + i];
     }
-    pipes::cols_x_p64(v_read[0] + off, v_read[1] + off, pf, o);
+    const uint32_t off = (uint32_t)(par * 2 * TILE);
+    pipes::cols_x_p64(va[0] + off, va[1] + off, pf, o);
   };
 
   if (t_begin < t_end) {
-    bool whole = is_whole(t_begin), next_whole = is_whole(t_begin + 1);
-    look_up(t_begin);
-    load(t_begin, whole);
-    look_up(t_begin + 1);
-    store(0, whole);
-    load(t_begin + 1, next_whole);
-    look_up(t_begin + 2);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    // Half of the waves convert the next tile before their matrix work, half of them after it: a SIMD has one of either
-    const bool early = (wave & 4) == 0;
-    int tile = t_begin, pair = 0;
-    auto step = [&](auto is_whole_tile) {
-      const bool more = tile + 1 < t_end, after_whole = is_whole(tile + 2);
-      auto advance = [&]() {
-        store(pair ^ 1, next_whole);
-        load(tile + 2, after_whole);  // (behind the last tile: some token of the sequence, not used)
-        look_up(tile + 3);
-      };
-      if (early && more) advance();
-      if (busy) compute(tile, pair, is_whole_tile);
-      if (!early && more) advance();
-      whole = next_whole;
-      next_whole = after_whole;
-      ++tile;
-      pair ^= 1;
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    };
-    while (tile < t_end) {
+    // K of the first two tiles and V of the first
+    {
+      KeyShare<D, G, N> k0;
+      const uint8_t* const run0 = run_of(look_up(t_begin));
+      const uint8_t* const run1 = run_of(look_up(t_begin + 1));
+      const uint8_t* const run2 = run_of(look_up(t_begin + 2));
+      k0.load(run0, page, slot_of(t_begin), part);
+      vt.load(run0, page, slot_of(t_begin), part);
+      kt.load(run1, page, slot_of(t_begin + 1), part);
+      store_k(k0, 0);
+      store_v(t_begin, 0);
+      store_k(kt, 1);
+      vt.load(run1, page, slot_of(t_begin + 1), part);
+      kt.load(run2, page, slot_of(t_begin + 2), part);
+      v_run = run2;
+      k_run = run_of(look_up(t_begin + 3));
+      next_page = look_up(t_begin + 4);
+    }
+    meet();
+    // Before every tile its K and V and the K of the one after it are in LDS.  Whole tiles come first, as a run of pipelined steps, each with
+    // P V of one tile and the logits of the next.
+    int tile = t_begin, par = 0;
+    if (tile < t_whole) {
+      pipes::PipeState st;
+      cache_pipes::pipe_start(0, ka, ab, qf, qb, m, l, c_row, st);
+      meet();  // its K may be overwritten
 #pragma unroll 1
-      while (tile < t_end && whole) step(std::true_type{});
-      if (tile < t_end) step(std::false_type{});
+      for (; tile < t_whole - 1; ++tile) {
+        advance(tile, par);
+        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row);
+        par ^= 1;
+        meet();
+      }
+      advance(tile, par);
+      cache_pipes::pipe_end(par, va, o, m, l, st, c_row);
+      ++tile;
+      par ^= 1;
+      meet();
+    }
+#pragma unroll 1
+    for (; tile < t_end; ++tile) {
+      masked_tile(tile, par);
+      meet();
+      advance(tile, par);
+      par ^= 1;
+      meet();
     }
   }
 
