@@ -26,10 +26,48 @@ def pv(D, half):
     return [dict(op=MFMA, **m) for m in base.pv_mfmas(D, half)]
 
 
+CONV_R = 216                # v[216:219]: 8 converted values on their way to LDS
+CONV_T = FS_T + 5           # two temporaries that the softmax streams leave alone
+
+
+def half_words(i, dst, src):
+    """two codes of word `src` as fp16 1 + c/16: channels i and i + 4"""
+    return [f"v_lshlrev_b32 {dst}, {6 - 4 * i}, {src}" if i < 2 else f"v_lshrrev_b32 {dst}, {4 * i - 6}, {src}",
+            f"v_and_or_b32 {dst}, {dst}, %[mask], %[one]"]
+
+
+def convert(D, n, k_slot, v_slot):
+    """n code words of K and of V, converted and written to LDS (KeyShare, ValueShare in pasa_cache_tile.hip)"""
+    r, t = [vr(CONV_R + i) for i in range(4)], [vr(CONV_T + i) for i in range(2)]
+    mix = lambda dst, src, hi: f"v_fma_mix_f32 {dst}, {src}, %[vs], %[vm] op_sel:[{hi},0,0] op_sel_hi:[1,0,0]"
+    pk = lambda dst, a, b: f"v_cvt_pk_bf16_f32 {dst}, {a}, {b}"
+    out = []
+    for j in range(n):
+        for i in range(4):
+            out += half_words(i, r[i], f"%[kc{j}]")
+            out.append(f"v_pk_fma_f16 {r[i]}, {r[i]}, %[ks{j}], %[km{j}]")
+        addr = "%[kst]"
+        if j:
+            out.append(f"v_xor_b32 {t[0]}, {hex(j << 6)}, %[kst]")
+            addr = t[0]
+        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(k_slot * 256 * D)}")
+    for j in range(n):
+        out += half_words(0, t[0], f"%[vc{j}]") + half_words(1, t[1], f"%[vc{j}]")
+        out += [mix(r[0], t[0], 0), mix(r[1], t[1], 0), mix(r[2], t[0], 1), mix(r[3], t[1], 1), pk(r[0], r[0], r[1]), pk(r[2], r[2], r[3])]
+        out += half_words(2, t[0], f"%[vc{j}]") + half_words(3, t[1], f"%[vc{j}]")
+        out += [mix(r[1], t[0], 0), mix(r[3], t[1], 0), pk(r[1], r[1], r[3]), mix(r[3], t[0], 1), mix(t[0], t[1], 1), pk(r[3], r[3], t[0])]
+        addr = "%[vst]"
+        if j:
+            out.append(f"v_xor_b32 {t[0]}, {hex(j << 4)}, %[vst]")
+            addr = t[0]
+        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(v_slot * 256 * D)}")
+    return out
+
+
 def run(D, mf, before, after, k_slot, v_slot, prologue=()):
     """MFMA k of `mf` with its operand fetch issued six MFMAs ahead (as pipe_run of gen_mfma_pipes.py); k_slot, v_slot: which of the two
-    K and V tiles of the ring"""
-    lines, issued, nbuf = [], [], 6
+    K and V tiles of the ring.  LDS instructions end in order, so a wait counts those issued after the one it waits for."""
+    lines, ends, count, nbuf = [], [], [0], 6
     k_off, b_off, v_off = k_slot * 256 * D, k_slot * 64 * BIAS_ROW, v_slot * 256 * D
 
     def issue(k):
@@ -42,27 +80,28 @@ def run(D, mf, before, after, k_slot, v_slot, prologue=()):
         else:
             lines.append(f"ds_read_b64_tr_b16 {base.Flo(f)}, %[va{2 * b}]{off(v_off + a * 32 * D)}")
             lines.append(f"ds_read_b64_tr_b16 {base.Fhi(f)}, %[va{2 * b + 1}]{off(v_off + a * 32 * D)}")
-        issued.append(2 if kind == "v" else 1)
+        count[0] += 2 if kind == "v" else 1
+        ends.append(count[0])
 
     n = len(mf)
     for k in range(min(nbuf, n)):
         issue(k)
     lines += list(prologue)
     for k in range(n):
-        outstanding = sum(issued[k + 1:])
-        assert outstanding <= 15
-        lines.append(f"s_waitcnt lgkmcnt({outstanding})")
+        lines.append(f"s_waitcnt lgkmcnt({min(count[0] - ends[k], 15)})")
         lines += before.get(k, [])
         m = mf[k]
         lines.append(f"{m['op']} {m['acc']}, {F(k % nbuf)}, {m['b']}, {'0' if m['first'] else m['acc']}")
         if k + nbuf < n:
             issue(k + nbuf)
         lines += after.get(k, [])
+        count[0] += sum(x.startswith("ds_") for x in after.get(k, []))
     return lines
 
 
-def pipe_step(D, par):
-    """P V of the tile in V slot par, logits of the next one, in the other K slot"""
+def pipe_step(D, words, par):
+    """P V of the tile in V slot par, logits of the next one, in the other K slot; K of the tile after that goes into slot par, V of the
+    next one into the other V slot"""
     n_o = 16 * (D // 32)
     mf = qk(D, 0) + pv(D, 0) + qk(D, 1) + pv(D, 1)
     n = len(mf)
@@ -75,6 +114,7 @@ def pipe_step(D, par):
     pour(after, n, max_stream(FS_S0) + [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S0, FS_P0), begin=0.5)
     k = n // 2 + 1  # the P V of the first half is through
     after[k] = list(pending(cold, "%[flag1]", corr1, n_o, "s_nop 3")) + after.get(k, [])
+    pour(after, n, convert(D, words, par, 1 - par))
     return run(D, mf, {}, after, 1 - par, par, prologue=max_stream(FS_S1)) + cold.text()
 
 
@@ -137,10 +177,18 @@ def gen():
              base.both_parities("pb", lambda par: pipe_start(D, par)),
              ml + ['"=&{v[184:199]}"(st.s1)'] + [x.replace("+", "=&") for x in pa] + ['[corr] "=&v"(st.corr)', '[flag] "=&s"(st.flag)'],
              kin + cin + par_in, list(s0) + list(p1) + rest)
-        emit("// P V of the tile in V slot par, logits of the next one, in the other K slot.  va: the lane's addresses of the column fragments in V slot 0\n",
-             f"pipe_step(int par, {k_args}, const uint32_t (&va)[{2 * nt}], {q_args}, {state}, float c)", "  uint64_t flag1;\n",
-             base.both_parities("ps", lambda par: pipe_step(D, par)),
-             base.o_ops(nt) + ml + [sb] + pa + carry + ['[flag1] "=&s"(flag1)'], kin + vin + cin + par_in, list(s0) + list(p1) + rest)
+        for words in (D // 64, D // 32):
+            conv = [f'[{x}{j}] "v"({x}[{j}])' for x in ("kc", "ks", "km", "vc") for j in range(words)] + \
+                [f'[{x}] "v"({x})' for x in ("vs", "vm", "kst", "vst")] + ['[mask] "v"(0x03c003c0u)', '[one] "s"(0x3c003c00u)']
+            arr = f"const uint32_t (&%s)[{words}]"
+            emit("// P V of the tile in V slot par, logits of the next one, in the other K slot.  va: the lane's addresses of the column fragments in V slot 0.\n"
+                 f"// Meanwhile {words} code words of K are converted and written to K slot par, and {words} of V to the other V slot: kc, vc the words, ks, km 16 s and\n"
+                 "// -24 s of a K word's group as two equal fp16 numbers, vs, vm 16 s and m - 16 s of the V words, kst, vst the lane's addresses in slots 0\n",
+                 f"pipe_step(int par, {k_args}, const uint32_t (&va)[{2 * nt}], {q_args}, {state}, float c,\n"
+                 f"                           {arr % 'kc'}, {arr % 'ks'}, {arr % 'km'}, {arr % 'vc'}, float vs, float vm, uint32_t kst, uint32_t vst)",
+                 "  uint64_t flag1;\n", base.both_parities("ps", lambda par: pipe_step(D, words, par)),
+                 base.o_ops(nt) + ml + [sb] + pa + carry + ['[flag1] "=&s"(flag1)'], kin + vin + cin + par_in + conv,
+                 list(s0) + list(p1) + list(range(CONV_R, CONV_R + 4)) + rest)
         emit("// End of a run: P V of the tile in V slot par\n",
              f"pipe_end(int par, const uint32_t (&va)[{2 * nt}], {state}, float c)", "", base.both_parities("pe", lambda par: pipe_end(D, par)),
              base.o_ops(nt) + ml + [sb] + pa + carry, vin + cin + par_in, list(s0) + list(p1) + rest)

@@ -85,30 +85,35 @@ struct KeyShare : Share<D, G, N> {
     load_words<S::KG>(at + 4 * (S::first_word(part) * 32 / G), par);
     bias = *reinterpret_cast<const uint32_t*>(at + 4 * min(S::quarter(part), L::NG - 1));
   }
-  // Into row `token` of the tile at `tile`.
-  // at_bias: the token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with
-  // (hi, lo, hi, 0) of the group's sum of q
-  PASA_DEVICE void store(char* tile, char* at_bias, int token, int part) const {
+  // The token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with (hi, lo, hi, 0) of
+  // the group's sum of q
+  PASA_DEVICE void store_bias(char* at, int token, int part) const {
     const int quarter = S::quarter(part);
-    {
-      const float mid = fmaf(8.f, bf16_low(bias), bf16_high(bias));
-      const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
-      const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
-      uint2 x = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
-      if (quarter >= L::NG) x = make_uint2(0u, 0u);
-      *reinterpret_cast<uint2*>(at_bias + token * 32 + quarter * 8) = x;
-    }
-    f16x2 a[S::KG], b[S::KG];
+    const float mid = fmaf(8.f, bf16_low(bias), bf16_high(bias));
+    const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
+    const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
+    uint2 x = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+    if (quarter >= L::NG) x = make_uint2(0u, 0u);
+    *reinterpret_cast<uint2*>(at + token * 32 + quarter * 8) = x;
+  }
+  // 16 s and -24 s of every word's group, as two equal fp16 numbers
+  PASA_DEVICE void factors(uint32_t (&a)[N], uint32_t (&b)[N]) const {
 #pragma unroll
-    for (int g = 0; g < S::KG; ++g) {
-      const float s = bf16_low(par[g]);
+    for (int j = 0; j < N; ++j) {
+      const float s = bf16_low(par[S::k_group(j)]);
       const _Float16 a1 = (_Float16)(16.f * s), b1 = (_Float16)(-24.f * s);
-      a[g] = f16x2{a1, a1};
-      b[g] = f16x2{b1, b1};
+      const f16x2 a2 = {a1, a1}, b2 = {b1, b1};
+      a[j] = __builtin_bit_cast(uint32_t, a2);
+      b[j] = __builtin_bit_cast(uint32_t, b2);
     }
+  }
+  static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, 4 * (S::first_word(part) + j) + S::quarter(part)); }
+  PASA_DEVICE void store(char* tile, int token, int part) const {
+    uint32_t a[N], b[N];
+    factors(a, b);
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, 4 * (S::first_word(part) + j) + quarter)) = keys8(code[j], a[S::k_group(j)], b[S::k_group(j)]);
+      *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = keys8(code[j], __builtin_bit_cast(f16x2, a[j]), __builtin_bit_cast(f16x2, b[j]));
   }
 };
 template <int D, int G, int N>
@@ -120,11 +125,12 @@ struct ValueShare : Share<D, G, N> {
     load_words<N>(run + L::v_codes(page) + slot * L::CODE + 4 * N * part, code);
     par = *reinterpret_cast<const uint32_t*>(run + L::v_params(page) + slot * L::PARAM + 4 * (8 * N * part / G));
   }
+  static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, N * part + j); }
   PASA_DEVICE void store(char* tile, int token, int part, bool hide) const {
     const uint32_t w = hide ? 0u : par;
     const float s = bf16_low(w), a = 16.f * s, b = bf16_high(w) - a;
 #pragma unroll
-    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(tile + lds_chunk_off<D>(token, N * part + j)) = values8(code[j], a, b);
+    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = values8(code[j], a, b);
   }
 };
 
@@ -253,7 +259,10 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   auto slot_of = [&](int tile) -> uint32_t { return (uint32_t)(64 * tile + token) & (page - 1u); };
   const uint8_t *k_run, *v_run;  // of the tiles to be requested next
   int next_page;                 // of the tile after k_run's
-  auto store_k = [&](const KeyShare<D, G, N>& share, int par) { share.store(ring + par * 2 * TILE, ring + 4 * TILE + par * BIAS, token, part); };
+  auto store_k = [&](const KeyShare<D, G, N>& share, int par) {
+    share.store_bias(ring + 4 * TILE + par * BIAS, token, part);
+    share.store(ring + par * 2 * TILE, token, part);
+  };
   // Weights of zero do not hide values that are not finite from the rows that do not see them: in a tile that is not whole such values
   // become zeros, and `bad` says so to the rows that do see the token (which are NaN throughout then, not only in the channels of that group)
   auto store_v = [&](int tile, int par) {
@@ -266,15 +275,18 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     }
     vt.store(ring + par * 2 * TILE + TILE, token, part, hide);
   };
-  // While tile t (in the slots par) is worked on: K of t + 2 and V of t + 1 into LDS
-  auto advance = [&](int t, int par) {
-    store_k(kt, par);
-    store_v(t + 1, par ^ 1);
+  // While tile t (in the slots par) is worked on, K of t + 2 and V of t + 1 are converted, and those after them requested
+  auto request = [&](int t) {
     kt.load(k_run, page, slot_of(t + 3), part);
     vt.load(v_run, page, slot_of(t + 2), part);
     v_run = k_run;
     k_run = run_of(next_page);
     next_page = look_up(t + 5);
+  };
+  auto advance = [&](int t, int par) {
+    store_k(kt, par);
+    store_v(t + 1, par ^ 1);
+    request(t);
   };
   auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
@@ -355,12 +367,20 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     int tile = t_begin, par = 0;
     if (tile < t_whole) {
       pipes::PipeState st;
+      const uint32_t kst = ring_base + (uint32_t)kt.lds_offset(token, part, 0), vst = ring_base + (uint32_t)(TILE + vt.lds_offset(token, part, 0));
       cache_pipes::pipe_start(0, ka, ab, qf, qb, m, l, c_row, st);
       meet();  // its K may be overwritten
 #pragma unroll 1
       for (; tile < t_whole - 1; ++tile) {
-        advance(tile, par);
-        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row);
+        // the conversion runs in the shadow of the matrix instructions
+        kt.store_bias(ring + 4 * TILE + par * BIAS, token, part);
+        uint32_t kc[N], ks[N], km[N], vc[N];
+        kt.factors(ks, km);
+        const float vs = 16.f * bf16_low(vt.par), vm = bf16_high(vt.par) - vs;
+#pragma unroll
+        for (int j = 0; j < N; ++j) { kc[j] = kt.code[j]; vc[j] = vt.code[j]; }
+        request(tile);
+        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row, kc, ks, km, vc, vs, vm, kst, vst);
         par ^= 1;
         meet();
       }
