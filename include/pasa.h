@@ -337,8 +337,7 @@ PASA_API int pasa_budget_schedule(const double* l1, int32_t n_prompts, int32_t n
  * cache stands for s c + m:
  *   m = smallest value of the group;  s = bf16(binary32((largest - m) / 15)), 0 if that is below 2^-126;
  *   c = (x - m) / s rounded to the nearest integer, ties to even, at most 15  (0 if s = 0).
- * A group that holds an infinity or a NaN reads back as NaN, and so does a group of K that holds a value beyond +-16384 (products with keys
- * are formed in binary16).
+ * A group that holds an infinity, a NaN or a value beyond +-16384 (K; its products are formed in binary16) or +-2^100 (V) reads back as NaN.
  * Bytes: the pool is [n_pages][H_kv] runs; a run is K codes [page][d/2], V codes [page][d/2], K parameters [page][d/group],
  * V parameters [page][d/group]; a parameter is s, then m.  A 32-bit word of codes holds 8 channels, channel i of them in bits
  * 4i .. 4i+3; word w of a token's V codes holds the channels 8w .. 8w+7, word q * (d/32) + j of its K codes the channels

@@ -27,40 +27,46 @@ def pv(D, half):
 
 
 CONV_R = 216                # v[216:219]: 8 converted values on their way to LDS
-CONV_T = FS_T + 5           # two temporaries that the softmax streams leave alone
-
-
-def half_words(i, dst, src):
-    """two codes of word `src` as fp16 1 + c/16: channels i and i + 4"""
-    return [f"v_lshlrev_b32 {dst}, {6 - 4 * i}, {src}" if i < 2 else f"v_lshrrev_b32 {dst}, {4 * i - 6}, {src}",
-            f"v_and_or_b32 {dst}, {dst}, %[mask], %[one]"]
+CONV_T = FS_T + 5           # three temporaries that the softmax streams leave alone
 
 
 def convert(D, n, k_slot, v_slot):
-    """n code words of K and of V, converted and written to LDS (KeyShare, ValueShare in pasa_cache_tile.hip)"""
-    r, t = [vr(CONV_R + i) for i in range(4)], [vr(CONV_T + i) for i in range(2)]
-    mix = lambda dst, src, hi: f"v_fma_mix_f32 {dst}, {src}, %[vs], %[vm] op_sel:[{hi},0,0] op_sel_hi:[1,0,0]"
-    pk = lambda dst, a, b: f"v_cvt_pk_bf16_f32 {dst}, {a}, {b}"
+    """n code words of K and of V, converted and written to LDS (keys8, values8 in pasa_cache_tile.hip)"""
+    r, t = [vr(CONV_R + i) for i in range(4)], [vr(CONV_T + i) for i in range(3)]
     out = []
-    for j in range(n):
-        for i in range(4):
-            out += half_words(i, r[i], f"%[kc{j}]")
-            out.append(f"v_pk_fma_f16 {r[i]}, {r[i]}, %[ks{j}], %[km{j}]")
-        addr = "%[kst]"
+
+    def write(base, j, shift, offset):
+        addr = f"%[{base}]"
         if j:
-            out.append(f"v_xor_b32 {t[0]}, {hex(j << 6)}, %[kst]")
+            out.append(f"v_xor_b32 {t[0]}, {hex(j << shift)}, {addr}")
             addr = t[0]
-        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(k_slot * 256 * D)}")
+        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(offset)}")
+
     for j in range(n):
-        out += half_words(0, t[0], f"%[vc{j}]") + half_words(1, t[1], f"%[vc{j}]")
-        out += [mix(r[0], t[0], 0), mix(r[1], t[1], 0), mix(r[2], t[0], 1), mix(r[3], t[1], 1), pk(r[0], r[0], r[1]), pk(r[2], r[2], r[3])]
-        out += half_words(2, t[0], f"%[vc{j}]") + half_words(3, t[1], f"%[vc{j}]")
-        out += [mix(r[1], t[0], 0), mix(r[3], t[1], 0), pk(r[1], r[1], r[3]), mix(r[3], t[0], 1), mix(t[0], t[1], 1), pk(r[3], r[3], t[0])]
-        addr = "%[vst]"
-        if j:
-            out.append(f"v_xor_b32 {t[0]}, {hex(j << 4)}, %[vst]")
-            addr = t[0]
-        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(v_slot * 256 * D)}")
+        for i in range(4):  # channels i and i + 4
+            out.append(f"v_lshlrev_b32 {r[i]}, {6 - 4 * i}, %[kc{j}]" if i < 2 else f"v_lshrrev_b32 {r[i]}, {4 * i - 6}, %[kc{j}]")
+            out.append(f"v_and_or_b32 {r[i]}, {r[i]}, %[mask], %[one]")
+            out.append(f"v_pk_fma_f16 {r[i]}, {r[i]}, %[ks{j}], %[km{j}] op_sel_hi:[1,0,0]")
+        write("kst", j, 6, k_slot * 256 * D)
+
+    def mix(dst, src, hi, b):
+        out.append(f"v_fma_mix_f32 {dst}, {src}, %[vs], %[vm{b}] op_sel:[{hi},0,0] op_sel_hi:[1,0,0]")
+
+    for j in range(n):
+        src = f"%[vc{j}]"
+        for i in range(2):  # channels 2 i, 2 i + 1 -> r[i]; 2 i + 4, 2 i + 5 -> r[i + 2]
+            out.append(f"v_and_or_b32 {t[1]}, {src}, %[high], %[c64]")
+            out.append(f"v_and_or_b32 {t[0]}, {src}, %[low], %[c1024]")  # (src may be t[0])
+            mix(r[i], t[0], 0, 0)
+            mix(t[2], t[1], 0, 1)
+            mix(r[i + 2], t[0], 1, 0)
+            out.append(f"v_cvt_pk_bf16_f32 {r[i]}, {r[i]}, {t[2]}")
+            mix(t[1], t[1], 1, 1)
+            if i == 0:  # the upper half of every 16 bits
+                out.append(f"v_lshrrev_b32 {t[0]}, 8, {src}")
+                src = t[0]
+            out.append(f"v_cvt_pk_bf16_f32 {r[i + 2]}, {r[i + 2]}, {t[1]}")
+        write("vst", j, 4, v_slot * 256 * D)
     return out
 
 
@@ -179,13 +185,15 @@ def gen():
              kin + cin + par_in, list(s0) + list(p1) + rest)
         for words in (D // 64, D // 32):
             conv = [f'[{x}{j}] "v"({x}[{j}])' for x in ("kc", "ks", "km", "vc") for j in range(words)] + \
-                [f'[{x}] "v"({x})' for x in ("vs", "vm", "kst", "vst")] + ['[mask] "v"(0x03c003c0u)', '[one] "s"(0x3c003c00u)']
+                [f'[{x}] "v"({x})' for x in ("vs", "vm0", "vm1", "kst", "vst")] + \
+                [f'[{n}] "{c}"({v})' for n, c, v in (("mask", "v", "0x03c003c0u"), ("one", "s", "0x3c003c00u"), ("low", "v", "0x000f000fu"),
+                                                     ("c1024", "s", "0x64006400u"), ("high", "v", "0x00f000f0u"), ("c64", "s", "0x54005400u"))]
             arr = f"const uint32_t (&%s)[{words}]"
             emit("// P V of the tile in V slot par, logits of the next one, in the other K slot.  va: the lane's addresses of the column fragments in V slot 0.\n"
                  f"// Meanwhile {words} code words of K are converted and written to K slot par, and {words} of V to the other V slot: kc, vc the words, ks, km 16 s and\n"
-                 "// -24 s of a K word's group as two equal fp16 numbers, vs, vm 16 s and m - 16 s of the V words, kst, vst the lane's addresses in slots 0\n",
+                 "// -24 s of a K word's group in fp16, vs, vm0, vm1 s, m - 1024 s and m - 64 s of the V words, kst, vst the lane's addresses in slots 0\n",
                  f"pipe_step(int par, {k_args}, const uint32_t (&va)[{2 * nt}], {q_args}, {state}, float c,\n"
-                 f"                           {arr % 'kc'}, {arr % 'ks'}, {arr % 'km'}, {arr % 'vc'}, float vs, float vm, uint32_t kst, uint32_t vst)",
+                 f"                           {arr % 'kc'}, {arr % 'ks'}, {arr % 'km'}, {arr % 'vc'}, float vs, float vm0, float vm1, uint32_t kst, uint32_t vst)",
                  "  uint64_t flag1;\n", base.both_parities("ps", lambda par: pipe_step(D, words, par)),
                  base.o_ops(nt) + ml + [sb] + pa + carry + ['[flag1] "=&s"(flag1)'], kin + vin + cin + par_in + conv,
                  list(s0) + list(p1) + list(range(CONV_R, CONV_R + 4)) + rest)

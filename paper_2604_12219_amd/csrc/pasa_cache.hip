@@ -8,7 +8,7 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr uint32_t kMostKey = 0x46800000u, kMostValue = 0x7f7fffffu;  // 16384; any finite number
+constexpr uint32_t kMostKey = 0x46800000u, kMostValue = 0x71800000u;  // 16384, 2^100
 
 template <int CTRL>
 PASA_DEVICE float dpp_f(float x) {

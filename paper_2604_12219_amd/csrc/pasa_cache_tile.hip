@@ -5,10 +5,11 @@
 // to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, so the wider one
 // (eight waves, 256 rows) pays half as much a row.
 //
-//   V: bf16(s c + m).  A shift and an and-or put two codes into fp16 numbers 1 + c/16, a mixed fma makes s c + m of each
-//     (16 s (1 + c/16) + (m - 16 s): the rounding of that is 2^-20 of s), a conversion rounds two of them to bf16: 2.5 instructions a value.
-//   K: fp16 s (c - 8), which is exact (s has 8 bits, c - 8 at most 3 or is a power of two), one packed fma for two codes: 1.5 instructions a
-//     value.  What that leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix instruction per 32 keys, with both factors as sums
+//   V: bf16(s c + m).  An and-or (and one shift for half of a word) makes fp16 numbers 1024 + c or 64 + c of two codes, a mixed fma
+//     s c + m of each (s (1024 + c) + (m - 1024 s): the rounding of that is 2^-13 of s), a conversion rounds two of them to bf16: 2.1 instructions a
+//     value.  Values beyond +-2^100 do not exist in a cache (pasa_cache_write), so 1024 s is finite.
+//   K: fp16 s (c - 8), which is exact (s has 8 bits, c - 8 at most 3 or is a power of two): a shift and an and-or make 1 + c/16 of two codes, a
+//     packed fma 16 s (1 + c/16) - 24 s: 1.5 instructions a value.  What that leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix instruction per 32 keys, with both factors as sums
 //     of two fp16 numbers (22 bits).  So the logits are those of the cache's values to binary32; with keys rounded to bf16 they are not,
 //     and lse is off by 1e-5.  Queries are fp16 times a power of two per row, which the row's logit scale takes back.
 //     Keys beyond +-16384 do not exist in a cache (pasa_cache_write), so 24 s is an fp16 number.
@@ -22,23 +23,31 @@ typedef __attribute__((address_space(4))) const int32_t const_i32;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// 8 values of a word of codes in bf16; a = 16 s, b = m - 16 s
-PASA_DEVICE uint4 values8(uint32_t x, float a, float b) {
-  const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 2) & 0x03c003c0u) | 0x3c003c00u,
-                         ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
-  float lo[4], hi[4];
+// 8 values of a word of codes in bf16; b0 = m - 1024 s, b1 = m - 64 s
+PASA_DEVICE uint4 values8(uint32_t x, float s, float b0, float b1) {
+  float v[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {  // channels i and i + 4
-    const f16x2 c = __builtin_bit_cast(f16x2, h[i]);
-    lo[i] = fmaf((float)c[0], a, b);
-    hi[i] = fmaf((float)c[1], a, b);
+  for (int i = 0; i < 2; ++i) {
+    const f16x2 a = __builtin_bit_cast(f16x2, ((x >> (8 * i)) & 0x000f000fu) | 0x64006400u);  // 1024 + c of channels 2 i and 2 i + 4
+    const f16x2 b = __builtin_bit_cast(f16x2, ((x >> (8 * i)) & 0x00f000f0u) | 0x54005400u);  // 64 + c of channels 2 i + 1 and 2 i + 5
+    v[2 * i] = fmaf((float)a[0], s, b0);
+    v[2 * i + 4] = fmaf((float)a[1], s, b0);
+    v[2 * i + 1] = fmaf((float)b[0], s, b1);
+    v[2 * i + 5] = fmaf((float)b[1], s, b1);
   }
-  const bf16x2 r[4] = {{(__bf16)lo[0], (__bf16)lo[1]}, {(__bf16)lo[2], (__bf16)lo[3]}, {(__bf16)hi[0], (__bf16)hi[1]}, {(__bf16)hi[2], (__bf16)hi[3]}};
-  return make_uint4(__builtin_bit_cast(uint32_t, r[0]), __builtin_bit_cast(uint32_t, r[1]), __builtin_bit_cast(uint32_t, r[2]), __builtin_bit_cast(uint32_t, r[3]));
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x2 p = {(__bf16)v[2 * i], (__bf16)v[2 * i + 1]};
+    r[i] = __builtin_bit_cast(uint32_t, p);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// 8 keys' values s (c - 8) of a word of codes in fp16, in the order 0 4 1 5 2 6 3 7; a = 16 s, b = -24 s (twice each)
-PASA_DEVICE uint4 keys8(uint32_t x, f16x2 a, f16x2 b) {
+// 8 keys' values s (c - 8) of a word of codes in fp16, in the order 0 4 1 5 2 6 3 7; a = 16 s, b = -24 s in fp16
+PASA_DEVICE uint4 keys8(uint32_t x, uint32_t a1, uint32_t b1) {
+  const f16x2 a = __builtin_shufflevector(__builtin_bit_cast(f16x2, a1), __builtin_bit_cast(f16x2, a1), 0, 0);
+  const f16x2 b = __builtin_shufflevector(__builtin_bit_cast(f16x2, b1), __builtin_bit_cast(f16x2, b1), 0, 0);
   const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 2) & 0x03c003c0u) | 0x3c003c00u,
                          ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
   uint32_t r[4];
@@ -48,16 +57,16 @@ PASA_DEVICE uint4 keys8(uint32_t x, f16x2 a, f16x2 b) {
 }
 
 template <int N>
-PASA_DEVICE void load_words(const uint8_t* at, uint32_t (&w)[N]) {
+PASA_DEVICE void load_words(const uint8_t* base, uint32_t off, uint32_t (&w)[N]) {
   if constexpr (N == 4) {
-    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    const uint4 v = *reinterpret_cast<const uint4*>(base + off);
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
   } else if constexpr (N == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(at);
+    const uint2 v = *reinterpret_cast<const uint2*>(base + off);
     w[0] = v.x; w[1] = v.y;
   } else {
     static_assert(N == 1, "");
-    w[0] = *reinterpret_cast<const uint32_t*>(at);
+    w[0] = *reinterpret_cast<const uint32_t*>(base + off);
   }
 }
 
@@ -65,11 +74,14 @@ PASA_DEVICE bool finite_param(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (
 
 // A thread's share of a tile: N code words of one token's K, and as many of its V, with the parameters they need.
 // `part` counts the threads of a token: they divide each quarter (the words of one q) of the K codes, and the V codes in order.
+// The tokens of a wave are 8 or 16 consecutive ones, all in one page: what depends on the page is scalar, the lane's offsets stay the same.
 template <int D, int G, int N>
 struct Share {
   typedef CacheLayout<D, G> L;
   static constexpr int PARTS = D / 8 / N, PER_Q = D / 32 / N;  // threads of a token, of a quarter
+  static constexpr int TOKENS = 64 / PARTS;                    // tokens of a wave
   static constexpr int KG = N * 32 > G ? N * 32 / G : 1;       // groups of a thread's K words
+  static_assert(16 % TOKENS == 0, "");
   static __device__ constexpr int k_group(int j) { return j * 32 / G; }  // of the j-th word, among them
   static PASA_DEVICE int quarter(int part) { return part / PER_Q; }
   static PASA_DEVICE int first_word(int part) { return part % PER_Q * N; }  // in its quarter
@@ -79,11 +91,20 @@ struct KeyShare : Share<D, G, N> {
   typedef Share<D, G, N> S;
   typedef typename S::L L;
   uint32_t code[N], par[S::KG], bias;  // bias: the parameter of group `quarter`
-  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, int part) {
-    load_words<N>(run + L::k_codes(page) + slot * L::CODE + 4 * (S::quarter(part) * (D / 32) + S::first_word(part)), code);
-    const uint8_t* const at = run + L::k_params(page) + slot * L::PARAM;
-    load_words<S::KG>(at + 4 * (S::first_word(part) * 32 / G), par);
-    bias = *reinterpret_cast<const uint32_t*>(at + 4 * min(S::quarter(part), L::NG - 1));
+  struct Offsets {
+    uint32_t code, par, bias;
+    PASA_DEVICE void init(int token, int part) {
+      code = token * L::CODE + 4 * (S::quarter(part) * (D / 32) + S::first_word(part));
+      par = token * L::PARAM + 4 * (S::first_word(part) * 32 / G);
+      bias = token * L::PARAM + 4 * min(S::quarter(part), L::NG - 1);
+    }
+  };
+  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, const Offsets& at) {  // run, slot: of the wave's first token
+    load_words<N>(run + (L::k_codes(page) + slot * L::CODE), at.code, code);
+    load_words<S::KG>(run + (L::k_params(page) + slot * L::PARAM), at.par, par);
+    uint32_t w[1];
+    load_words<1>(run + (L::k_params(page) + slot * L::PARAM), at.bias, w);
+    bias = w[0];
   }
   // The token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with (hi, lo, hi, 0) of
   // the group's sum of q
@@ -96,13 +117,12 @@ struct KeyShare : Share<D, G, N> {
     if (quarter >= L::NG) x = make_uint2(0u, 0u);
     *reinterpret_cast<uint2*>(at + token * 32 + quarter * 8) = x;
   }
-  // 16 s and -24 s of every word's group, as two equal fp16 numbers
+  // 16 s and -24 s of every word's group as fp16 numbers, in the low halves
   PASA_DEVICE void factors(uint32_t (&a)[N], uint32_t (&b)[N]) const {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float s = bf16_low(par[S::k_group(j)]);
-      const _Float16 a1 = (_Float16)(16.f * s), b1 = (_Float16)(-24.f * s);
-      const f16x2 a2 = {a1, a1}, b2 = {b1, b1};
+      const f16x2 a2 = {(_Float16)(16.f * s), (_Float16)0.f}, b2 = {(_Float16)(-24.f * s), (_Float16)0.f};
       a[j] = __builtin_bit_cast(uint32_t, a2);
       b[j] = __builtin_bit_cast(uint32_t, b2);
     }
@@ -113,7 +133,7 @@ struct KeyShare : Share<D, G, N> {
     factors(a, b);
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = keys8(code[j], __builtin_bit_cast(f16x2, a[j]), __builtin_bit_cast(f16x2, b[j]));
+      *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = keys8(code[j], a[j], b[j]);
   }
 };
 template <int D, int G, int N>
@@ -121,16 +141,31 @@ struct ValueShare : Share<D, G, N> {
   typedef Share<D, G, N> S;
   typedef typename S::L L;
   uint32_t code[N], par;
-  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, int part) {
-    load_words<N>(run + L::v_codes(page) + slot * L::CODE + 4 * N * part, code);
-    par = *reinterpret_cast<const uint32_t*>(run + L::v_params(page) + slot * L::PARAM + 4 * (8 * N * part / G));
+  struct Offsets {
+    uint32_t code, par;
+    PASA_DEVICE void init(int token, int part) {
+      code = token * L::CODE + 4 * N * part;
+      par = token * L::PARAM + 4 * (8 * N * part / G);
+    }
+  };
+  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, const Offsets& at) {
+    load_words<N>(run + (L::v_codes(page) + slot * L::CODE), at.code, code);
+    uint32_t w[1];
+    load_words<1>(run + (L::v_params(page) + slot * L::PARAM), at.par, w);
+    par = w[0];
+  }
+  // what values8 takes: s, m - 1024 s, m - 64 s
+  static PASA_DEVICE void factors(uint32_t par, float& s, float& b0, float& b1) {
+    s = bf16_low(par);
+    b0 = fmaf(-1024.f, s, bf16_high(par));
+    b1 = fmaf(-64.f, s, bf16_high(par));
   }
   static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, N * part + j); }
   PASA_DEVICE void store(char* tile, int token, int part, bool hide) const {
-    const uint32_t w = hide ? 0u : par;
-    const float s = bf16_low(w), a = 16.f * s, b = bf16_high(w) - a;
+    float s, b0, b1;
+    factors(hide ? 0u : par, s, b0, b1);
 #pragma unroll
-    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = values8(code[j], a, b);
+    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = values8(code[j], s, b0, b1);
   }
 };
 
@@ -232,9 +267,13 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   }
 
   // ---- how a tile gets into LDS ----
-  const int token = tid / S::PARTS, part = tid % S::PARTS;
+  const int token0 = wave * S::TOKENS, token = token0 + lane / S::PARTS, part = tid % S::PARTS;
   KeyShare<D, G, N> kt;
   ValueShare<D, G, N> vt;
+  typename KeyShare<D, G, N>::Offsets k_at;
+  typename ValueShare<D, G, N>::Offsets v_at;
+  k_at.init(lane / S::PARTS, part);
+  v_at.init(lane / S::PARTS, part);
   auto is_page = [&](int pg) -> bool { return pg >= 0 && pg < p.c.n_pages; };
   // Whether all pages of the workgroup's tokens are followed (or else every tile is masked: `followed` below looks each of them up)
   bool pages_good = true;
@@ -250,13 +289,13 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     return bits;
   };
   const int t_whole = pages_good ? max(min(limit_all >> 6, t_end), t_begin) : t_begin;  // before it every row sees every token
-  // A token's page is looked up a step before its codes are requested, these a step before they are converted.  (Behind the last tile: some
-  // token of the sequence, converted and not used)
+  // The page of a wave's tokens is looked up a step before their codes are requested, these a step before they are converted.  (Behind the last
+  // tile: some tokens of the sequence, converted and not used)
   const int64_t pool_page = (int64_t)p.c.H_kv * p.c.head_bytes;
   const uint8_t* const pool_head = p.c.pool + (int64_t)hkv * p.c.head_bytes;
-  auto look_up = [&](int tile) -> int { return p.c.pages[(int64_t)b * p.c.max_pages + (min(64 * tile + token, seq.length - 1) >> p.c.log_page)]; };
+  auto look_up = [&](int tile) -> int { return table[min(64 * tile + token0, seq.length - 1) >> p.c.log_page]; };
   auto run_of = [&](int pg) -> const uint8_t* { return pool_head + (is_page(pg) ? pg : 0) * pool_page; };
-  auto slot_of = [&](int tile) -> uint32_t { return (uint32_t)(64 * tile + token) & (page - 1u); };
+  auto slot_of = [&](int tile) -> uint32_t { return (uint32_t)(64 * tile + token0) & (page - 1u); };
   const uint8_t *k_run, *v_run;  // of the tiles to be requested next
   int next_page;                 // of the tile after k_run's
   auto store_k = [&](const KeyShare<D, G, N>& share, int par) {
@@ -277,8 +316,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   };
   // While tile t (in the slots par) is worked on, K of t + 2 and V of t + 1 are converted, and those after them requested
   auto request = [&](int t) {
-    kt.load(k_run, page, slot_of(t + 3), part);
-    vt.load(v_run, page, slot_of(t + 2), part);
+    kt.load(k_run, page, slot_of(t + 3), k_at);
+    vt.load(v_run, page, slot_of(t + 2), v_at);
     v_run = k_run;
     k_run = run_of(next_page);
     next_page = look_up(t + 5);
@@ -349,14 +388,14 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
       const uint8_t* const run0 = run_of(look_up(t_begin));
       const uint8_t* const run1 = run_of(look_up(t_begin + 1));
       const uint8_t* const run2 = run_of(look_up(t_begin + 2));
-      k0.load(run0, page, slot_of(t_begin), part);
-      vt.load(run0, page, slot_of(t_begin), part);
-      kt.load(run1, page, slot_of(t_begin + 1), part);
+      k0.load(run0, page, slot_of(t_begin), k_at);
+      vt.load(run0, page, slot_of(t_begin), v_at);
+      kt.load(run1, page, slot_of(t_begin + 1), k_at);
       store_k(k0, 0);
       store_v(t_begin, 0);
       store_k(kt, 1);
-      vt.load(run1, page, slot_of(t_begin + 1), part);
-      kt.load(run2, page, slot_of(t_begin + 2), part);
+      vt.load(run1, page, slot_of(t_begin + 1), v_at);
+      kt.load(run2, page, slot_of(t_begin + 2), k_at);
       v_run = run2;
       k_run = run_of(look_up(t_begin + 3));
       next_page = look_up(t_begin + 4);
@@ -376,11 +415,12 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
         kt.store_bias(ring + 4 * TILE + par * BIAS, token, part);
         uint32_t kc[N], ks[N], km[N], vc[N];
         kt.factors(ks, km);
-        const float vs = 16.f * bf16_low(vt.par), vm = bf16_high(vt.par) - vs;
+        float vs, vm0, vm1;
+        vt.factors(vt.par, vs, vm0, vm1);
 #pragma unroll
         for (int j = 0; j < N; ++j) { kc[j] = kt.code[j]; vc[j] = vt.code[j]; }
         request(tile);
-        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row, kc, ks, km, vc, vs, vm, kst, vst);
+        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row, kc, ks, km, vc, vs, vm0, vm1, kst, vst);
         par ^= 1;
         meet();
       }

@@ -10,7 +10,7 @@ def token_bytes(d, group):
     return d + 8 * (d // group)
 
 
-MOST_KEY = 16384.0
+MOST_KEY, MOST_VALUE = 16384.0, 2.0 ** 100
 
 
 def quantise(x, group, most=math.inf):
@@ -71,7 +71,7 @@ class Model:
                 for h in range(self.H_kv):
                     run = self.run(pg, h)
                     for is_key, x in ((True, k), (False, v)):
-                        c, s, m = quantise(x[b, h, i], self.group, MOST_KEY if is_key else math.inf)
+                        c, s, m = quantise(x[b, h, i], self.group, MOST_KEY if is_key else MOST_VALUE)
                         byte, shift = self.code_place(is_key)
                         code = torch.zeros(d // 2, dtype=torch.long).index_add_(0, byte, c.cpu() << shift)
                         at = (0 if is_key else page * d // 2) + slot * (d // 2)
