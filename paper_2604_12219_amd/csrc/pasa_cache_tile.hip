@@ -108,14 +108,14 @@ struct KeyShare : Share<D, G, N> {
   }
   // The token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with (hi, lo, hi, 0) of
   // the group's sum of q
-  PASA_DEVICE void store_bias(char* at, int token, int part) const {
+  PASA_DEVICE uint2 offsets(int part) const {
     const int quarter = S::quarter(part);
     const float mid = fmaf(8.f, bf16_low(bias), bf16_high(bias));
     const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
     const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
     uint2 x = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
     if (quarter >= L::NG) x = make_uint2(0u, 0u);
-    *reinterpret_cast<uint2*>(at + token * 32 + quarter * 8) = x;
+    return x;
   }
   // 16 s and -24 s of every word's group as fp16 numbers, in the low halves
   PASA_DEVICE void factors(uint32_t (&a)[N], uint32_t (&b)[N]) const {
@@ -128,13 +128,6 @@ struct KeyShare : Share<D, G, N> {
     }
   }
   static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, 4 * (S::first_word(part) + j) + S::quarter(part)); }
-  PASA_DEVICE void store(char* tile, int token, int part) const {
-    uint32_t a[N], b[N];
-    factors(a, b);
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = keys8(code[j], a[j], b[j]);
-  }
 };
 template <int D, int G, int N>
 struct ValueShare : Share<D, G, N> {
@@ -161,12 +154,6 @@ struct ValueShare : Share<D, G, N> {
     b1 = fmaf(-64.f, s, bf16_high(par));
   }
   static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, N * part + j); }
-  PASA_DEVICE void store(char* tile, int token, int part, bool hide) const {
-    float s, b0, b1;
-    factors(hide ? 0u : par, s, b0, b1);
-#pragma unroll
-    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(tile + lds_offset(token, part, j)) = values8(code[j], s, b0, b1);
-  }
 };
 
 template <int D, int G, int WAVES>
@@ -298,34 +285,56 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   auto slot_of = [&](int tile) -> uint32_t { return (uint32_t)(64 * tile + token0) & (page - 1u); };
   const uint8_t *k_run, *v_run;  // of the tiles to be requested next
   int next_page;                 // of the tile after k_run's
-  auto store_k = [&](const KeyShare<D, G, N>& share, int par) {
-    share.store_bias(ring + 4 * TILE + par * BIAS, token, part);
-    share.store(ring + par * 2 * TILE, token, part);
+  // What a step converts: K of the tile two further down, V of the next one
+  struct {
+    uint32_t kc[N], ks[N], km[N], vc[N], v_par;
+    float vs, vm0, vm1;
+    uint2 bias;
+  } cv;
+  auto take_k = [&](const KeyShare<D, G, N>& share) {
+    share.factors(cv.ks, cv.km);
+    cv.bias = share.offsets(part);
+#pragma unroll
+    for (int j = 0; j < N; ++j) cv.kc[j] = share.code[j];
   };
-  // Weights of zero do not hide values that are not finite from the rows that do not see them: in a tile that is not whole such values
-  // become zeros, and `bad` says so to the rows that do see the token (which are NaN throughout then, not only in the channels of that group)
-  auto store_v = [&](int tile, int par) {
-    bool hide = false;
-    if (tile >= t_whole) {
-      const bool finite = finite_param(vt.par);
-      hide = !finite || 64 * tile + token >= limit_any || (!pages_good && !is_page(look_up(tile)));
-      const uint64_t not_finite = __builtin_amdgcn_ballot_w64(!finite) >> (lane & ~(S::PARTS - 1));
-      if (part == 0) bad[par][token] = (not_finite & ((1u << S::PARTS) - 1u)) ? NAN : 0.f;
-    }
-    vt.store(ring + par * 2 * TILE + TILE, token, part, hide);
+  auto take_v = [&]() {
+    cv.v_par = vt.par;
+    vt.factors(vt.par, cv.vs, cv.vm0, cv.vm1);
+#pragma unroll
+    for (int j = 0; j < N; ++j) cv.vc[j] = vt.code[j];
   };
-  // While tile t (in the slots par) is worked on, K of t + 2 and V of t + 1 are converted, and those after them requested
-  auto request = [&](int t) {
+  auto take = [&](int t) {  // for the step of tile t; what comes after that is requested
+    take_k(kt);
+    take_v();
     kt.load(k_run, page, slot_of(t + 3), k_at);
     vt.load(v_run, page, slot_of(t + 2), v_at);
     v_run = k_run;
     k_run = run_of(next_page);
     next_page = look_up(t + 5);
   };
-  auto advance = [&](int t, int par) {
-    store_k(kt, par);
+  auto store_bias = [&](int par) { *reinterpret_cast<uint2*>(ring + 4 * TILE + par * BIAS + token * 32 + S::quarter(part) * 8) = cv.bias; };
+  auto store_k = [&](int par) {
+    store_bias(par);
+#pragma unroll
+    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(ring + par * 2 * TILE + kt.lds_offset(token, part, j)) = keys8(cv.kc[j], cv.ks[j], cv.km[j]);
+  };
+  // Weights of zero do not hide values that are not finite from the rows that do not see them: in a tile that is not whole such values
+  // become zeros, and `bad` says so to the rows that do see the token (which are NaN throughout then, not only in the channels of that group)
+  auto store_v = [&](int tile, int par) {
+    if (tile >= t_whole) {
+      const bool finite = finite_param(cv.v_par);
+      const bool hide = !finite || 64 * tile + token >= limit_any || (!pages_good && !is_page(look_up(tile)));
+      const uint64_t not_finite = __builtin_amdgcn_ballot_w64(!finite) >> (lane & ~(S::PARTS - 1));
+      if (part == 0) bad[par][token] = (not_finite & ((1u << S::PARTS) - 1u)) ? NAN : 0.f;
+      if (hide) vt.factors(0u, cv.vs, cv.vm0, cv.vm1);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      *reinterpret_cast<uint4*>(ring + par * 2 * TILE + TILE + vt.lds_offset(token, part, j)) = values8(cv.vc[j], cv.vs, cv.vm0, cv.vm1);
+  };
+  auto store = [&](int t, int par) {  // what was taken for tile t, which is in the slots par
+    store_k(par);
     store_v(t + 1, par ^ 1);
-    request(t);
   };
   auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
@@ -391,9 +400,12 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
       k0.load(run0, page, slot_of(t_begin), k_at);
       vt.load(run0, page, slot_of(t_begin), v_at);
       kt.load(run1, page, slot_of(t_begin + 1), k_at);
-      store_k(k0, 0);
+      take_k(k0);
+      store_k(0);
+      take_k(kt);
+      store_k(1);
+      take_v();
       store_v(t_begin, 0);
-      store_k(kt, 1);
       vt.load(run1, page, slot_of(t_begin + 1), v_at);
       kt.load(run2, page, slot_of(t_begin + 2), k_at);
       v_run = run2;
@@ -408,23 +420,18 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
       pipes::PipeState st;
       const uint32_t kst = ring_base + (uint32_t)kt.lds_offset(token, part, 0), vst = ring_base + (uint32_t)(TILE + vt.lds_offset(token, part, 0));
       cache_pipes::pipe_start(0, ka, ab, qf, qb, m, l, c_row, st);
-      meet();  // its K may be overwritten
+      meet();  // the first K may be overwritten
 #pragma unroll 1
       for (; tile < t_whole - 1; ++tile) {
+        take(tile);
+        store_bias(par);
         // the conversion runs in the shadow of the matrix instructions
-        kt.store_bias(ring + 4 * TILE + par * BIAS, token, part);
-        uint32_t kc[N], ks[N], km[N], vc[N];
-        kt.factors(ks, km);
-        float vs, vm0, vm1;
-        vt.factors(vt.par, vs, vm0, vm1);
-#pragma unroll
-        for (int j = 0; j < N; ++j) { kc[j] = kt.code[j]; vc[j] = vt.code[j]; }
-        request(tile);
-        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row, kc, ks, km, vc, vs, vm0, vm1, kst, vst);
+        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row, cv.kc, cv.ks, cv.km, cv.vc, cv.vs, cv.vm0, cv.vm1, kst, vst);
         par ^= 1;
         meet();
       }
-      advance(tile, par);
+      take(tile);
+      store(tile, par);
       cache_pipes::pipe_end(par, va, o, m, l, st, c_row);
       ++tile;
       par ^= 1;
@@ -434,7 +441,8 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     for (; tile < t_end; ++tile) {
       masked_tile(tile, par);
       meet();
-      advance(tile, par);
+      take(tile);
+      store(tile, par);
       par ^= 1;
       meet();
     }
