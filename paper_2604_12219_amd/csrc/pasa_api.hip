@@ -777,26 +777,37 @@ int cache_rows_params(const void* k, const void* v, const pasa_shape_t* shape, c
   p.n = shape->n;
   return PASA_OK;
 }
-// the rows of a key/value head's query heads are numbered in 32 bits, with room for a last incomplete workgroup and for the splits
-bool cache_rows_fit(const pasa_shape_t* s, const pasa_cache_t* c) { return (int64_t)(s->H / c->H_kv) * s->n <= ((int64_t)1 << 30); }
+// the rows of a key/value head's query heads are numbered in 32 bits, with room for a last incomplete workgroup and for the splits, and so are
+// the runs of 128 of them of all sequences
+bool cache_rows_fit(const pasa_shape_t* s, const pasa_cache_t* c) {
+  const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
+  return rows <= ((int64_t)1 << 30) && s->B * ((rows + 127) / 128) < ((int64_t)1 << 31) - 1024;
+}
 
 // How the rows and tokens of a call are divided among workgroups, and the workspace that takes
 struct CacheAttnPlan {
-  int wg_rows, splits;
-  size_t part_ml, total;
+  int wg_rows, splits, pieces, row_tiles;
+  size_t part_ml, merge, total;
 };
 CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int32_t n_max) {
   CacheAttnPlan a{};
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
   a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 32 ? 16 : rows <= 128 ? 128 : 256;
-  const int64_t resident = a.wg_rows <= 16 ? 768 : a.wg_rows == 128 ? 512 : 256;
-  const int64_t wgs = (int64_t)s->B * c->H_kv * ((rows + a.wg_rows - 1) / a.wg_rows);
   a.splits = 1;
-  while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= resident && tokens >= (a.splits + 1) * 512) ++a.splits;
-  const size_t parts = a.splits > 1 ? (size_t)s->B * s->H * s->n * a.splits : 0;
+  size_t parts = 0;
+  if (a.wg_rows <= 16) {
+    const int64_t wgs = (int64_t)s->B * c->H_kv * ((rows + a.wg_rows - 1) / a.wg_rows);
+    while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= 768 && tokens >= (a.splits + 1) * 512) ++a.splits;
+    if (a.splits > 1) parts = (size_t)s->B * s->H * s->n * a.splits;
+  } else {
+    a.pieces = a.wg_rows == 128 ? 512 : 256;  // as many as can be resident on 256 compute units
+    a.row_tiles = (int)((rows + a.wg_rows - 1) / a.wg_rows);
+    parts = (size_t)2 * a.pieces * a.wg_rows;
+  }
   a.part_ml = align_up(parts * s->d * 4);
-  a.total = align_up(a.part_ml + parts * 2 * 4 + 1);  // never zero: that means "invalid"
+  a.merge = align_up(a.part_ml + parts * 2 * 4);
+  a.total = align_up(a.merge + a.pieces * sizeof(CacheMerge) + 1);  // never zero: that means "invalid"
   return a;
 }
 }  // namespace
@@ -847,6 +858,8 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   p.wg_rows = plan.wg_rows; p.splits = plan.splits;
   p.part_o = static_cast<float*>(ws);
   p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.part_ml);
+  p.pieces = plan.pieces; p.row_tiles = plan.row_tiles;
+  p.merge = reinterpret_cast<CacheMerge*>(static_cast<char*>(ws) + plan.merge);
   return pasa_launch_cache_attn(p, static_cast<hipStream_t>(stream)) == hipSuccess ? PASA_OK : PASA_EHIP;
 }
 

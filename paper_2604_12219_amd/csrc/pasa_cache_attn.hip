@@ -417,7 +417,8 @@ hipError_t launch_rows(const CacheAttnParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream) {
-  const hipError_t rc = p.wg_rows >= 128 ? pasa_launch_cache_tiles(p, stream) : launch_rows(p, stream);
+  if (p.wg_rows >= 128) return pasa_launch_cache_tiles(p, stream);
+  const hipError_t rc = launch_rows(p, stream);
   if (rc != hipSuccess || p.splits == 1) return rc;
   const dim3 grid((p.n + 3) / 4, p.H, p.c.B);
   if (p.c.d == 64) cache_merge_kernel<64><<<grid, 256, 0, stream>>>(p);

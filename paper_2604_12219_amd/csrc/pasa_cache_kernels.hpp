@@ -23,6 +23,9 @@ struct CacheRowsParams {  // write: K and V rows -> cache; read: cache -> rows
 hipError_t pasa_launch_cache_write(const CacheRowsParams& p, hipStream_t stream);
 hipError_t pasa_launch_cache_read(const CacheRowsParams& p, hipStream_t stream);
 
+struct CacheMerge {  // an item that several workgroups of cache_tile_kernel share (pasa_cache_tile.hip)
+  int32_t hkv, item, first_slot, parts;  // parts = 0: none
+};
 struct CacheAttnParams {
   CacheParams c;
   const uint16_t* q;
@@ -32,10 +35,15 @@ struct CacheAttnParams {
   int32_t H, n, causal;
   float scale;  // of the logits, times log2(e)
   int32_t wg_rows;  // (row, head of a key/value head's share) pairs of a workgroup: 4, 8, 16 (pasa_cache_attn.hip), 128 or 256 (pasa_cache_tile.hip)
-  int32_t splits;   // workgroups among which a sequence's tokens are divided, at most kCacheMaxSplits
-  float* part_o;    // splits > 1: fp32 [B][H][n][splits][d], sums against the maximum of their split
-  float* part_ml;   //             fp32 [B][H][n][splits][2], that maximum (log2 units) and the sum of the weights
+  // 4, 8, 16: a sequence's tokens are divided among `splits` workgroups, at most kCacheMaxSplits, and with splits > 1
+  int32_t splits;
+  float* part_o;   // fp32 [B][H][n][splits][d]: sums against the maximum of their split
+  float* part_ml;  // fp32 [B][H][n][splits][2]: that maximum (log2 units) and the sum of the weights
+  // 128, 256: all the work is divided among `pieces` workgroups; part_o, part_ml are [2 pieces][wg_rows][d], [..][2]
+  int32_t pieces, row_tiles;  // row_tiles = runs of wg_rows rows that a sequence can have
+  CacheMerge* merge;          // [pieces]
 };
+constexpr int kCacheMinPiece = 8;  // tiles: less is not worth sharing an item
 constexpr int kCacheMaxSplits = 64;  // a wave of the merging kernel holds one per lane
-hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // the attention kernel alone
+hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // wg_rows 128 or 256
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);

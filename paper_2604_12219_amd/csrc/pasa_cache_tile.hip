@@ -156,6 +156,53 @@ struct ValueShare : Share<D, G, N> {
   static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, N * part + j); }
 };
 
+// ---- who does what ----
+// An item is a (sequence, run of ROWS rows), numbered e = b * row_tiles + run, of one key/value head; its weight is the number of tiles that its rows
+// see (at least one where there are rows: somebody has to write them).  All items of all heads in a row, head by head, are a line of
+// tiles that the workgroups divide evenly, each a piece of `piece` of them: so an item can be shared by several workgroups, and the last ones have no
+// less to do than the first, whatever the lengths are (they are known on the device only).  Against one workgroup an item: 40 heads of 15 items,
+// 600 workgroups on 256 compute units, 7640 -> us.
+// A workgroup's piece holds at most two parts of items: one at its start (slot 2 w of the partial results) and one at its end (slot 2 w + 1).
+struct CacheItem {
+  int b, row0, rows;  // rows: of the sequence, times the share of heads
+  CacheSequence seq;
+};
+PASA_DEVICE CacheItem cache_item(const CacheAttnParams& p, int e) {
+  CacheItem it;
+  it.b = e / p.row_tiles;
+  it.row0 = (e % p.row_tiles) * p.wg_rows;
+  it.seq = cache_sequence(p.c, it.b, p.n);
+  it.rows = p.H / p.c.H_kv * it.seq.rows;
+  return it;
+}
+PASA_DEVICE int row_limit(const CacheAttnParams& p, const CacheSequence& seq, int r) {  // tokens that row r sees
+  if (!p.causal) return seq.length;
+  const int64_t own = seq.first + r / (p.H / p.c.H_kv) + 1;
+  return own < 0 ? 0 : own < seq.length ? (int)own : seq.length;
+}
+PASA_DEVICE int item_tiles(const CacheAttnParams& p, const CacheItem& it) { return (row_limit(p, it.seq, min(it.row0 + p.wg_rows, it.rows) - 1) + 63) >> 6; }
+PASA_DEVICE int item_weight(const CacheAttnParams& p, int e) {
+  const CacheItem it = cache_item(p, e);
+  return it.row0 >= it.rows ? 0 : max(item_tiles(p, it), 1);
+}
+// the first item from e on that has rows (p.c.B * row_tiles if there is none)
+PASA_DEVICE int next_item(const CacheAttnParams& p, int e) {
+  const int end = p.c.B * p.row_tiles;
+  while (e < end) {
+    const CacheItem it = cache_item(p, e);
+    if (it.row0 < it.rows) return e;
+    e = (it.b + 1) * p.row_tiles;
+  }
+  return end;
+}
+PASA_DEVICE int64_t wave_inclusive_sum(int64_t x, int lane) {
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up((long long)x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
 template <int D, int G, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnParams p) {
   typedef CacheLayout<D, G> L;
@@ -167,21 +214,57 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   __shared__ __attribute__((aligned(1024))) char ring[4 * TILE + 2 * BIAS];  // K, V of one tile, K, V of the next; offset operands of either
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
 
-  // the last rows first: with a causal mask they have the most to do
-  const int row_tiles = gridDim.x / p.splits;
-  const int split = blockIdx.x % p.splits, row0 = (row_tiles - 1 - (int)(blockIdx.x / p.splits)) * ROWS, hkv = blockIdx.y, b = blockIdx.z;
-  const CacheSequence seq = cache_sequence(p.c, b, p.n);
-  const int share = p.H / p.c.H_kv, rows = share * seq.rows;
-  if (row0 >= rows) return;
-  const int last_row = min(row0 + ROWS, rows) - 1;
-  auto limit_of = [&](int r) -> int {  // tokens that row r sees
-    if (!p.causal) return seq.length;
-    const int64_t own = seq.first + r / share + 1;
-    return own < 0 ? 0 : own < seq.length ? (int)own : seq.length;
-  };
-  const int limit_all = __builtin_amdgcn_readfirstlane(limit_of(row0)), limit_any = __builtin_amdgcn_readfirstlane(limit_of(last_row));
-  const int tiles = (limit_any + 63) >> 6, per = (tiles + p.splits - 1) / p.splits;
-  const int t_begin = __builtin_amdgcn_readfirstlane(split * per), t_end = __builtin_amdgcn_readfirstlane(min(tiles, (split + 1) * per));
+  // ---- this workgroup's piece ----
+  __shared__ int64_t s_sum[WAVES], s_at[2];
+  const int items = p.c.B * p.row_tiles;
+  int64_t head_tiles = 0;  // of one key/value head
+  for (int e = tid; e < items; e += WAVES * 64) head_tiles += item_weight(p, e);
+  head_tiles = wave_inclusive_sum(head_tiles, lane);
+  if (lane == 63) s_sum[wave] = head_tiles;
+  __syncthreads();
+  head_tiles = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) head_tiles += s_sum[w];
+  const int64_t all_tiles = head_tiles * p.c.H_kv, piece = max((all_tiles + gridDim.x - 1) / gridDim.x, (int64_t)kCacheMinPiece);
+  int64_t at = blockIdx.x * piece;
+  const int64_t end = min(at + piece, all_tiles);
+  if (tid == 0) p.merge[blockIdx.x].parts = 0;
+  if (at >= end) return;
+  int hkv = (int)(at / head_tiles), item = 0, off = 0;  // where the piece starts: tile `off` of the item
+  {
+    const int64_t want = at - hkv * head_tiles;
+    int64_t before = 0;  // tiles of the items before e0
+    for (int e0 = 0;; e0 += WAVES * 64) {
+      const int e = e0 + tid, weight = e < items ? item_weight(p, e) : 0;
+      const int64_t incl = wave_inclusive_sum(weight, lane);
+      __syncthreads();  // s_sum has been read
+      if (lane == 63) s_sum[wave] = incl;
+      __syncthreads();
+      int64_t first = before + incl - weight, all = before;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) first += s_sum[w];
+        all += s_sum[w];
+      }
+      if (want >= first && want < first + weight) { s_at[0] = e; s_at[1] = want - first; }
+      if (want < all) break;
+      before = all;
+    }
+    __syncthreads();
+    item = __builtin_amdgcn_readfirstlane((int)s_at[0]);
+    off = __builtin_amdgcn_readfirstlane((int)s_at[1]);
+    hkv = __builtin_amdgcn_readfirstlane(hkv);
+  }
+
+  for (bool first_part = true; at < end; first_part = false) {
+  const CacheItem it = cache_item(p, item);
+  const int b = it.b, row0 = it.row0, rows = it.rows, share = p.H / p.c.H_kv, last_row = min(row0 + ROWS, rows) - 1;
+  const CacheSequence seq = it.seq;
+  const int limit_all = __builtin_amdgcn_readfirstlane(row_limit(p, seq, row0)), limit_any = __builtin_amdgcn_readfirstlane(row_limit(p, seq, last_row));
+  const int tiles = (limit_any + 63) >> 6, weight = max(tiles, 1);
+  const int take_tiles = (int)min((int64_t)(weight - off), end - at);
+  const int t_begin = __builtin_amdgcn_readfirstlane(min(off, tiles)), t_end = __builtin_amdgcn_readfirstlane(min(off + take_tiles, tiles));
+  const bool whole_item = take_tiles == weight;
   const uint32_t page = 1u << p.c.log_page;
   const_i32* const table = (const_i32*)(p.c.pages + (int64_t)b * p.c.max_pages);
 
@@ -189,7 +272,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   const int row = row0 + wave * 32 + ql;
   const int own = min(row, last_row), i_own = own / share, h_own = hkv * share + own % share;
   const int64_t row_off = b * p.stride_b + h_own * p.stride_h + i_own * p.stride_n;
-  const int limit = limit_of(own);
+  const int limit = row_limit(p, seq, own);
   // q / 2^e in fp16, 2^e the power of two at the row's largest magnitude, in the order of a word's codes; qb: the groups' sums of that
   f16x8 qf[D / 16], qb;
   float c_row;  // logit scale times log2(e) times 2^e
@@ -449,36 +532,95 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   }
 
   l = half_swap_sum(l);
-  if (row > last_row) return;
-  const int64_t line = ((int64_t)b * p.H + h_own) * p.n + i_own;
-  if (p.splits == 1) {  // a row that sees nothing is zero, its normaliser empty
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (row <= last_row) {
+    const int64_t line = ((int64_t)b * p.H + h_own) * p.n + i_own;
+    if (whole_item) {  // a row that sees nothing is zero, its normaliser empty
+      const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+      for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const bf16x2 x0 = {(__bf16)(o[t][4 * g] * inv), (__bf16)(o[t][4 * g + 1] * inv)};
-        const bf16x2 x1 = {(__bf16)(o[t][4 * g + 2] * inv), (__bf16)(o[t][4 * g + 3] * inv)};
-        *reinterpret_cast<uint2*>(p.o + row_off + 32 * t + 8 * g + 4 * h) = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+        for (int g = 0; g < 4; ++g) {
+          const bf16x2 x0 = {(__bf16)(o[t][4 * g] * inv), (__bf16)(o[t][4 * g + 1] * inv)};
+          const bf16x2 x1 = {(__bf16)(o[t][4 * g + 2] * inv), (__bf16)(o[t][4 * g + 3] * inv)};
+          *reinterpret_cast<uint2*>(p.o + row_off + 32 * t + 8 * g + 4 * h) = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+        }
+      if (p.lse && h == 0) p.lse[line] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    } else {
+      const int64_t part_row = (2 * blockIdx.x + (first_part ? 0 : 1)) * (int64_t)ROWS + (row - row0);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(p.part_o + part_row * D + 32 * t + 8 * g + 4 * h) = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
+      if (h == 0) { p.part_ml[2 * part_row] = m; p.part_ml[2 * part_row + 1] = l; }
+    }
+  }
+  if (tid == 0 && !whole_item && off + take_tiles == weight) {  // the last part of a shared item: cache_merge_items puts it together
+    const int64_t start = at - off;
+    const int w0 = (int)(start / piece);
+    p.merge[blockIdx.x] = {hkv, item, 2 * w0 + (start % piece != 0 ? 1 : 0), (int)blockIdx.x - w0 + 1};
+  }
+  at += take_tiles;
+  off = 0;
+  item = next_item(p, item + 1);
+  if (item == items) {
+    ++hkv;
+    item = next_item(p, 0);
+  }
+  item = __builtin_amdgcn_readfirstlane(item);
+  }
+}
+
+// Items that several workgroups share, from their parts: workgroup (w, y) handles rows 16 y .. of the item whose last part workgroup w of cache_tile_kernel
+// had.  A wave takes a row at a time.
+template <int D>
+__global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
+  const CacheMerge mg = p.merge[blockIdx.x];
+  if (mg.parts == 0) return;
+  const CacheItem it = cache_item(p, mg.item);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = p.H / p.c.H_kv;
+  for (int x = wave; x < 16; x += 4) {
+    const int r = blockIdx.y * 16 + x, row = it.row0 + r;
+    if (row >= it.rows) return;
+    // part 0 in slot first_slot, the others at the starts of the workgroups after that
+    auto slot = [&](int j) -> int64_t { return j == 0 ? mg.first_slot : (int64_t)2 * (mg.first_slot / 2 + j); };
+    float top = -INFINITY;
+    for (int j = lane; j < mg.parts; j += 64) top = fmaxf(top, p.part_ml[2 * (slot(j) * p.wg_rows + r)]);
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, o[D / 64] = {};
+    for (int j0 = 0; j0 < mg.parts; j0 += 64) {
+      float f = 0.f;
+      if (j0 + lane < mg.parts) {
+        const float* const ml = p.part_ml + 2 * (slot(j0 + lane) * p.wg_rows + r);
+        f = __builtin_amdgcn_exp2f(ml[0] - ref);
+        sum = fmaf(f, ml[1], sum);
       }
-    if (p.lse && h == 0) p.lse[line] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-  } else {
-    const int64_t part = line * p.splits + split;
+      const int count = min(64, mg.parts - j0);
+      for (int j = 0; j < count; ++j) {
+        const float fj = __shfl(f, j);
+        const float* const src = p.part_o + (slot(j0 + j) * p.wg_rows + r) * D + lane;
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+        for (int t = 0; t < D / 64; ++t) o[t] = fmaf(fj, src[64 * t], o[t]);
+      }
+    }
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    const int i = row / share, h = mg.hkv * share + row % share;
+    uint16_t* const out = p.o + it.b * p.stride_b + h * p.stride_h + i * p.stride_n;
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4*>(p.part_o + part * D + 32 * t + 8 * g + 4 * h) = make_float4(o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]);
-    if (h == 0) { p.part_ml[2 * part] = m; p.part_ml[2 * part + 1] = l; }
+    for (int t = 0; t < D / 64; ++t) {
+      const __bf16 y = (__bf16)(sum == 0.f ? 0.f : o[t] / sum);
+      out[64 * t + lane] = __builtin_bit_cast(uint16_t, y);
+    }
+    if (p.lse && lane == 0) p.lse[((int64_t)it.b * p.H + h) * p.n + i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
 }
 
 template <int D, int G>
 hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
-  const int rows = p.H / p.c.H_kv * p.n;
-  const dim3 grid((rows + p.wg_rows - 1) / p.wg_rows * p.splits, p.c.H_kv, p.c.B);
-  if (p.wg_rows == 128) cache_tile_kernel<D, G, 4><<<grid, 256, 0, stream>>>(p);
-  else cache_tile_kernel<D, G, 8><<<grid, 512, 0, stream>>>(p);
+  if (p.wg_rows == 128) cache_tile_kernel<D, G, 4><<<p.pieces, 256, 0, stream>>>(p);
+  else cache_tile_kernel<D, G, 8><<<p.pieces, 512, 0, stream>>>(p);
+  cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 16), 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
