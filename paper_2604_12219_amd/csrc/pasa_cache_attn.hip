@@ -369,33 +369,39 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
   }
 }
 
-// out and lse of a row from the results of its splits; one wave a row
+// out and lse of a row from the results of its splits: a workgroup a row, each wave every fourth split
 template <int D>
 __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttnParams p) {
-  const int lane = threadIdx.x & 63, i = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
+  __shared__ float part[4][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const CacheSequence seq = cache_sequence(p.c, b, p.n);
   if (i >= seq.rows) return;
-  const int64_t row = ((int64_t)b * p.H + h) * p.n + i, part = row * p.splits;
+  const int64_t row = ((int64_t)b * p.H + h) * p.n + i, first = row * p.splits;
   float m = -INFINITY, l = 0.f;
-  if (lane < p.splits) { m = p.part_ml[2 * (part + lane)]; l = p.part_ml[2 * (part + lane) + 1]; }
+  if (lane < p.splits) { m = p.part_ml[2 * (first + lane)]; l = p.part_ml[2 * (first + lane) + 1]; }
   float top = m;
   for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
   float sum = f * l;
   for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
   float o[D / 64] = {};
-  for (int s = 0; s < p.splits; ++s) {
-    const float fs = __shfl(f, s);
+  const float* const src = p.part_o + first * D + lane;
+#pragma unroll 8
+  for (int s = wave; s < p.splits; s += 4) {
+    const float fs = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f), s));
 #pragma unroll
-    for (int t = 0; t < D / 64; ++t) o[t] = fmaf(fs, p.part_o[(part + s) * D + 64 * t + lane], o[t]);
+    for (int t = 0; t < D / 64; ++t) o[t] = fmaf(fs, src[s * D + 64 * t], o[t]);
   }
-  uint16_t* const out = p.o + b * p.stride_b + h * p.stride_h + i * p.stride_n;
 #pragma unroll
-  for (int t = 0; t < D / 64; ++t) {
-    const __bf16 y = (__bf16)(sum == 0.f ? 0.f : o[t] / sum);
-    out[64 * t + lane] = __builtin_bit_cast(uint16_t, y);
+  for (int t = 0; t < D / 64; ++t) part[wave][64 * t + lane] = o[t];
+  __syncthreads();
+  const int ch = threadIdx.x;
+  if (ch < D) {
+    const float val = (part[0][ch] + part[1][ch]) + (part[2][ch] + part[3][ch]);
+    const __bf16 y = (__bf16)(sum == 0.f ? 0.f : val / sum);
+    p.o[b * p.stride_b + h * p.stride_h + i * p.stride_n + ch] = __builtin_bit_cast(uint16_t, y);
   }
-  if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  if (p.lse && threadIdx.x == 0) p.lse[row] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int D, int G>
@@ -420,7 +426,7 @@ hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream) 
   if (p.wg_rows >= 128) return pasa_launch_cache_tiles(p, stream);
   const hipError_t rc = launch_rows(p, stream);
   if (rc != hipSuccess || p.splits == 1) return rc;
-  const dim3 grid((p.n + 3) / 4, p.H, p.c.B);
+  const dim3 grid(p.n, p.H, p.c.B);
   if (p.c.d == 64) cache_merge_kernel<64><<<grid, 256, 0, stream>>>(p);
   else cache_merge_kernel<128><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();

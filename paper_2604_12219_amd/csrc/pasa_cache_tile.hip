@@ -571,56 +571,55 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   }
 }
 
-// Items that several workgroups share, from their parts: workgroup (w, y) handles rows 16 y .. of the item whose last part workgroup w of cache_tile_kernel
-// had.  A wave takes a row at a time.
+// Items that several workgroups share, from their parts: workgroup (w, y) handles rows 4 y .. of the item whose last part workgroup w of cache_tile_kernel
+// had, a row a wave.
 template <int D>
 __global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
   const CacheMerge mg = p.merge[blockIdx.x];
   if (mg.parts == 0) return;
   const CacheItem it = cache_item(p, mg.item);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = p.H / p.c.H_kv;
-  for (int x = wave; x < 16; x += 4) {
-    const int r = blockIdx.y * 16 + x, row = it.row0 + r;
-    if (row >= it.rows) return;
-    // part 0 in slot first_slot, the others at the starts of the workgroups after that
-    auto slot = [&](int j) -> int64_t { return j == 0 ? mg.first_slot : (int64_t)2 * (mg.first_slot / 2 + j); };
-    float top = -INFINITY;
-    for (int j = lane; j < mg.parts; j += 64) top = fmaxf(top, p.part_ml[2 * (slot(j) * p.wg_rows + r)]);
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, o[D / 64] = {};
-    for (int j0 = 0; j0 < mg.parts; j0 += 64) {
-      float f = 0.f;
-      if (j0 + lane < mg.parts) {
-        const float* const ml = p.part_ml + 2 * (slot(j0 + lane) * p.wg_rows + r);
-        f = __builtin_amdgcn_exp2f(ml[0] - ref);
-        sum = fmaf(f, ml[1], sum);
-      }
-      const int count = min(64, mg.parts - j0);
-      for (int j = 0; j < count; ++j) {
-        const float fj = __shfl(f, j);
-        const float* const src = p.part_o + (slot(j0 + j) * p.wg_rows + r) * D + lane;
-#pragma unroll
-        for (int t = 0; t < D / 64; ++t) o[t] = fmaf(fj, src[64 * t], o[t]);
-      }
+  const int lane = threadIdx.x & 63, share = p.H / p.c.H_kv;
+  const int r = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), row = it.row0 + r;
+  if (row >= it.rows) return;
+  // part 0 in slot first_slot, the others at the starts of the workgroups after that
+  auto place = [&](int j) -> int64_t { return (j == 0 ? mg.first_slot : (int64_t)2 * (mg.first_slot / 2 + j)) * p.wg_rows + r; };
+  float top = -INFINITY;
+  for (int j = lane; j < mg.parts; j += 64) top = fmaxf(top, p.part_ml[2 * place(j)]);
+  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o[D / 64] = {};
+  for (int j0 = 0; j0 < mg.parts; j0 += 64) {
+    float f = 0.f;
+    if (j0 + lane < mg.parts) {
+      const float* const ml = p.part_ml + 2 * place(j0 + lane);
+      f = __builtin_amdgcn_exp2f(ml[0] - ref);
+      sum = fmaf(f, ml[1], sum);
     }
-    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-    const int i = row / share, h = mg.hkv * share + row % share;
-    uint16_t* const out = p.o + it.b * p.stride_b + h * p.stride_h + i * p.stride_n;
+    const int count = min(64, mg.parts - j0);
+#pragma unroll 4
+    for (int j = 0; j < count; ++j) {
+      const float fj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f), j));
+      const float* const src = p.part_o + place(j0 + j) * D + lane;
 #pragma unroll
-    for (int t = 0; t < D / 64; ++t) {
-      const __bf16 y = (__bf16)(sum == 0.f ? 0.f : o[t] / sum);
-      out[64 * t + lane] = __builtin_bit_cast(uint16_t, y);
+      for (int t = 0; t < D / 64; ++t) o[t] = fmaf(fj, src[64 * t], o[t]);
     }
-    if (p.lse && lane == 0) p.lse[((int64_t)it.b * p.H + h) * p.n + i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
+  for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+  const int i = row / share, h = mg.hkv * share + row % share;
+  uint16_t* const out = p.o + it.b * p.stride_b + h * p.stride_h + i * p.stride_n;
+#pragma unroll
+  for (int t = 0; t < D / 64; ++t) {
+    const __bf16 y = (__bf16)(sum == 0.f ? 0.f : o[t] / sum);
+    out[64 * t + lane] = __builtin_bit_cast(uint16_t, y);
+  }
+  if (p.lse && lane == 0) p.lse[((int64_t)it.b * p.H + h) * p.n + i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int D, int G>
 hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
   if (p.wg_rows == 128) cache_tile_kernel<D, G, 4><<<p.pieces, 256, 0, stream>>>(p);
   else cache_tile_kernel<D, G, 8><<<p.pieces, 512, 0, stream>>>(p);
-  cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 16), 256, 0, stream>>>(p);
+  cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 4), 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 

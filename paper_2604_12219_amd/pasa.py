@@ -461,31 +461,34 @@ def cache_attn_workspace_bytes(shape: Shape, cache: Cache, n_max: int = 0) -> in
     return load_library().pasa_cache_attn_workspace_bytes(ctypes.byref(shape.c()), ctypes.byref(cache.c()), n_max)
 
 
-def _check_cache_args(shape: Shape, cache: Cache, pool, pages, length, n_new, rows: dict):
-    """what the library cannot see: types, sizes, layouts and devices of the tensors behind the pointers"""
-    want = (shape.B, shape.H, shape.n, shape.d)
-    for name, t in rows.items():
-        if tuple(t.shape) != want:
+def _check_cache_args(shape: Shape, cache: Cache, pool, pages, length, n_new, rows):
+    """what the library cannot see: types, sizes, layouts and devices of the tensors behind the pointers.  (One pass of cheap comparisons; a
+    call of a few microseconds is mostly this.)"""
+    want, strides = (shape.B, shape.H, shape.n, shape.d), (shape.stride_b, shape.stride_h, shape.stride_n, 1)
+    for name, t in rows:
+        if t.shape != want:
             raise ValueError(f"{name}: expected {list(want)} as the shape says, got {list(t.shape)}")
-    _check_extent(shape, **rows)
-    _check_strides(shape, **rows)
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"{name}: expected bf16, got {t.dtype}")
+        if t.stride() != strides:  # with the strides of the shape a tensor lies inside its storage
+            _check_strides(shape, **{name: t})
     if pool.dtype != torch.uint8 or not pool.is_contiguous():
         raise ValueError("pool: expected a contiguous uint8 tensor")
-    for name, t, size in (("pages", pages, (shape.B, cache.max_pages)), ("length", length, (shape.B,)), ("n_new", n_new, (shape.B,))):
-        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != size or not t.is_contiguous()):
+    batch = (shape.B,)
+    for name, t, size in (("pages", pages, (shape.B, cache.max_pages)), ("length", length, batch), ("n_new", n_new, batch)):
+        if t is not None and (t.dtype != torch.int32 or t.shape != size or not t.is_contiguous()):
             raise ValueError(f"{name}: expected a contiguous int32 tensor of size {list(size)}")
-    here = torch.cuda.current_device() if pool.is_cuda else -1
-    for name, t in dict(rows, pool=pool, pages=pages, length=length, n_new=n_new).items():
-        if t is not None and (not t.is_cuda or t.get_device() != here):
-            raise ValueError(f"{name}: lies on {t.device}; every tensor has to be on the current GPU")
+    here = torch.cuda.current_device() if pool.is_cuda else -2
+    if any(t is not None and t.get_device() != here for t in (rows[0][1], rows[1][1], pool, pages, length, n_new)):
+        raise ValueError("every tensor has to be on the current GPU")
 
 
 def cache_write(k, v, shape: Shape, cache: Cache, pool, pages, length, n_new=None):
     """quantises row i < n_new[b] of k, v [B, H_kv, n, d] into the cache as token length[b] - n_new[b] + i of sequence b (n_new None: all n
     rows).  pool uint8 [cache_bytes(cache)], pages int32 [B, max_pages], length and n_new int32 [B], see pasa.h"""
-    _check_cache_args(shape, cache, pool, pages, length, n_new, {"k": k, "v": v})
-    _check(load_library().pasa_cache_write(_ptr(k), _ptr(v), ctypes.byref(shape.c()), ctypes.byref(cache.c()), _ptr(pool), pool.numel(), _ptr(pages),
-                                           _ptr(length), _ptr(n_new), _stream()), "pasa_cache_write")
+    _check_cache_args(shape, cache, pool, pages, length, n_new, (("k", k), ("v", v)))
+    _check(load_library().pasa_cache_write(k.data_ptr(), v.data_ptr(), ctypes.byref(shape.c()), ctypes.byref(cache.c()), pool.data_ptr(), pool.numel(),
+                                           pages.data_ptr(), length.data_ptr(), _ptr(n_new), _stream()), "pasa_cache_write")
 
 
 def cache_read(shape: Shape, cache: Cache, pool, pages, length, n_new=None, k=None, v=None):
@@ -494,7 +497,7 @@ def cache_read(shape: Shape, cache: Cache, pool, pages, length, n_new=None, k=No
     if k is None or v is None:
         full = torch.zeros((2, shape.B, shape.H, shape.n, shape.d), dtype=torch.bfloat16, device=pool.device)
         k, v = (full[0] if k is None else k), (full[1] if v is None else v)
-    _check_cache_args(shape, cache, pool, pages, length, n_new, {"k": k, "v": v})
+    _check_cache_args(shape, cache, pool, pages, length, n_new, (("k", k), ("v", v)))
     _check(load_library().pasa_cache_read(ctypes.byref(shape.c()), ctypes.byref(cache.c()), _ptr(pool), pool.numel(), _ptr(pages), _ptr(length),
                                           _ptr(n_new), _ptr(k), _ptr(v), _stream()), "pasa_cache_read")
     return k, v
@@ -509,7 +512,7 @@ def cache_attn(q, shape: Shape, cache: Cache, pool, pages, length, n_new=None, c
         out = torch.zeros_like(q)
     if lse is None and want_lse:
         lse = torch.zeros((shape.B * shape.H, shape.n), dtype=torch.float32, device=q.device)
-    _check_cache_args(shape, cache, pool, pages, length, n_new, {"q": q, "out": out})
+    _check_cache_args(shape, cache, pool, pages, length, n_new, (("q", q), ("out", out)))
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() != shape.B * shape.H * shape.n or not lse.is_contiguous() or
                             lse.get_device() != q.get_device()):
         raise ValueError(f"lse: expected a contiguous fp32 tensor of size {[shape.B * shape.H, shape.n]} beside q")
