@@ -16,38 +16,38 @@ MFMA_F16 = "v_mfma_f32_32x32x16_f16"
 BIAS_ROW = 32  # bytes of a key's offset operands
 
 
-def qk(D, half):
+def qk(D, half, tile=0):
     acc = vr(FS_S0 if half == 0 else FS_S1, 16)
-    return [dict(op=MFMA_F16, acc=acc, first=True, b="%[qb]", load=("b", 0, half))] + \
-        [dict(op=MFMA_F16, acc=acc, first=False, b=f"%[q{st}]", load=("k", st, half)) for st in range(D // 16)]
+    return [dict(op=MFMA_F16, acc=acc, first=True, b="%[qb]", load=("b", 0, half, tile))] + \
+        [dict(op=MFMA_F16, acc=acc, first=False, b=f"%[q{st}]", load=("k", st, half, tile)) for st in range(D // 16)]
 
 
-def pv(D, half):
-    return [dict(op=MFMA, **m) for m in base.pv_mfmas(D, half)]
+def pv(D, half, tile=0):
+    return [dict(op=MFMA, **dict(m, load=(*m["load"], tile))) for m in base.pv_mfmas(D, half)]
 
 
 CONV_R = 216                # v[216:219]: 8 converted values on their way to LDS
 CONV_T = FS_T + 5           # three temporaries that the softmax streams leave alone
 
 
-def convert(D, n, k_slot, v_slot):
-    """n code words of K and of V, converted and written to LDS (keys8, values8 in pasa_cache_tile.hip)"""
+def convert(D, n, group):
+    """n code words of K and of V, converted and written to the tiles `group` (keys8, values8 in pasa_cache_tile.hip)"""
     r, t = [vr(CONV_R + i) for i in range(4)], [vr(CONV_T + i) for i in range(3)]
     out = []
 
-    def write(base, j, shift, offset):
-        addr = f"%[{base}]"
+    def write(name, j, shift):
+        addr = f"%[{name}]"
         if j:
             out.append(f"v_xor_b32 {t[0]}, {hex(j << shift)}, {addr}")
             addr = t[0]
-        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(offset)}")
+        out.append(f"ds_write_b128 {addr}, {vr(CONV_R, 4)}{off(group * 2 * 128 * D)}")
 
     for j in range(n):
         for i in range(4):  # channels i and i + 4
             out.append(f"v_lshlrev_b32 {r[i]}, {6 - 4 * i}, %[kc{j}]" if i < 2 else f"v_lshrrev_b32 {r[i]}, {4 * i - 6}, %[kc{j}]")
             out.append(f"v_and_or_b32 {r[i]}, {r[i]}, %[mask], %[one]")
-            out.append(f"v_pk_fma_f16 {r[i]}, {r[i]}, %[ks{j}], %[km{j}] op_sel_hi:[1,0,0]")
-        write("kst", j, 6, k_slot * 256 * D)
+            out.append(f"v_pk_fma_f16 {r[i]}, {r[i]}, %[kf{j}], %[kf{j}] op_sel:[0,0,1] op_sel_hi:[1,0,1]")
+        write("kst", j, 6)
 
     def mix(dst, src, hi, b):
         out.append(f"v_fma_mix_f32 {dst}, {src}, %[vs], %[vm{b}] op_sel:[{hi},0,0] op_sel_hi:[1,0,0]")
@@ -66,26 +66,26 @@ def convert(D, n, k_slot, v_slot):
                 out.append(f"v_lshrrev_b32 {t[0]}, 8, {src}")
                 src = t[0]
             out.append(f"v_cvt_pk_bf16_f32 {r[i + 2]}, {r[i + 2]}, {t[1]}")
-        write("vst", j, 4, v_slot * 256 * D)
+        write("vst", j, 4)
     return out
 
 
-def run(D, mf, before, after, k_slot, v_slot, prologue=()):
-    """MFMA k of `mf` with its operand fetch issued six MFMAs ahead (as pipe_run of gen_mfma_pipes.py); k_slot, v_slot: which of the two
-    K and V tiles of the ring.  LDS instructions end in order, so a wait counts those issued after the one it waits for."""
+def run(D, mf, before, after, group=0, prologue=()):
+    """MFMA k of `mf` with its operand fetch issued six MFMAs ahead (as pipe_run of gen_mfma_pipes.py), from a group of two tiles of the ring.
+    LDS instructions end in order, so a wait counts those issued after the one it waits for."""
     lines, ends, count, nbuf = [], [], [0], 6
-    k_off, b_off, v_off = k_slot * 256 * D, k_slot * 64 * BIAS_ROW, v_slot * 256 * D
 
     def issue(k):
         f = k % nbuf
-        kind, a, b = mf[k]["load"]
+        kind, a, b, tile = mf[k]["load"]
+        at = (2 * group + tile) * 128 * D
         if kind == "b":  # offset operands of 32 keys
-            lines.append(f"ds_read_b128 {F(f)}, %[ab]{off(b_off + b * 32 * BIAS_ROW)}")
+            lines.append(f"ds_read_b128 {F(f)}, %[ab]{off((2 * (2 * group + tile) + b) * 32 * BIAS_ROW)}")
         elif kind == "k":
-            lines.append(f"ds_read_b128 {F(f)}, %[ka{a}]{off(k_off + b * 64 * D)}")
+            lines.append(f"ds_read_b128 {F(f)}, %[ka{a}]{off(at + b * 64 * D)}")
         else:
-            lines.append(f"ds_read_b64_tr_b16 {base.Flo(f)}, %[va{2 * b}]{off(v_off + a * 32 * D)}")
-            lines.append(f"ds_read_b64_tr_b16 {base.Fhi(f)}, %[va{2 * b + 1}]{off(v_off + a * 32 * D)}")
+            lines.append(f"ds_read_b64_tr_b16 {base.Flo(f)}, %[va{2 * b}]{off(at + a * 32 * D)}")
+            lines.append(f"ds_read_b64_tr_b16 {base.Fhi(f)}, %[va{2 * b + 1}]{off(at + a * 32 * D)}")
         count[0] += 2 if kind == "v" else 1
         ends.append(count[0])
 
@@ -105,45 +105,60 @@ def run(D, mf, before, after, k_slot, v_slot, prologue=()):
     return lines
 
 
-def pipe_step(D, words, par):
-    """P V of the tile in V slot par, logits of the next one, in the other K slot; K of the tile after that goes into slot par, V of the
-    next one into the other V slot"""
-    n_o = 16 * (D // 32)
-    mf = qk(D, 0) + pv(D, 0) + qk(D, 1) + pv(D, 1)
-    n = len(mf)
-    cold = Cold(f"ps{par}_")
+def step_streams(after, n, at, n_o, cold):
+    """what runs beside the n MFMAs (from number `at` on) of a step: logits of 32 keys -> S0, P V with P0, logits -> S1, P V with P1; meanwhile the softmax of
+    what S1 held before -> P1 and of S0 -> P0 (the pipelined step of gen_mfma_pipes.py)"""
     corr1 = vr(FS_T + 3)
-    after = {}
-    after[1] = list(pending(cold, "%[flag]", "%[corr]", n_o, "s_nop 3"))  # left by the step before
+    late = {}
+    late[1] = list(pending(cold, "%[flag]", "%[corr]", n_o, "s_nop 3"))  # left by the step before
     # (done with S1 before the MFMAs of the second half write it; S0 is long complete)
-    pour(after, n, [growth(cold, "%[flag1]", corr1)] + exp_stream(FS_S1, FS_P1), first=1, end=0.5)
-    pour(after, n, max_stream(FS_S0) + [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S0, FS_P0), begin=0.5)
+    first = [growth(cold, "%[flag1]", corr1)] + exp_stream(FS_S1, FS_P1)
+    if at:  # the maximum of S1: at the start of the statement it has no MFMA to run beside
+        first = max_stream(FS_S1) + first
+    pour(late, n, first, first=0 if at else 1, end=0.5)
+    pour(late, n, max_stream(FS_S0) + [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S0, FS_P0), begin=0.5)
     k = n // 2 + 1  # the P V of the first half is through
-    after[k] = list(pending(cold, "%[flag1]", corr1, n_o, "s_nop 3")) + after.get(k, [])
-    pour(after, n, convert(D, words, par, 1 - par))
-    return run(D, mf, {}, after, 1 - par, par, prologue=max_stream(FS_S1)) + cold.text()
+    late[k] = list(pending(cold, "%[flag1]", corr1, n_o, "s_nop 3")) + late.get(k, [])
+    for k, x in late.items():
+        after.setdefault(at + k, []).extend(x)
 
 
-def pipe_start(D, par):
-    """logits of the tile in K slot par and the softmax of its first half"""
+def pipe_steps(D, words, group, tiles):
+    """for each of the tiles: P V of it, logits of the next one; its V is the tile of this number in the V group, the next one's K in the K group.
+    words > 0: meanwhile the other groups are filled"""
+    n_o = 16 * (D // 32)
+    mf, after, text = [], {}, []
+    for tile in range(tiles):
+        part = qk(D, 0, tile) + pv(D, 0, tile) + qk(D, 1, tile) + pv(D, 1, tile)
+        cold = Cold(f"ps{group}_{tile}_")
+        step_streams(after, len(part), len(mf), n_o, cold)
+        mf += part
+        text.append(cold)
+    if words:
+        pour(after, len(mf), convert(D, words, 1 - group))
+    return run(D, mf, {}, after, group, prologue=max_stream(FS_S1)) + sum([c.text() for c in text], [])
+
+
+def pipe_start(D):
+    """logits of a tile and the softmax of its first half"""
     mf = qk(D, 0) + qk(D, 1)
     n, q = len(mf), len(mf) // 2
-    cold = Cold(f"pb{par}_")
+    cold = Cold("pb")
     after = {}
     pour(after, n, max_stream(FS_S0) + [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S0, FS_P0), first=q + 1, begin=(q + 1) / n)
-    return run(D, mf, {}, after, par, 0) + [NOP_AFTER] + cold.text()
+    return run(D, mf, {}, after) + [NOP_AFTER] + cold.text()
 
 
-def pipe_end(D, par):
-    """P V of the last tile (V slot par) and the softmax of its second half"""
+def pipe_end(D):
+    """P V of the last tile and the softmax of its second half"""
     n_o = 16 * (D // 32)
     mf = pv(D, 0) + pv(D, 1)
     q = len(mf) // 2
-    cold = Cold(f"pe{par}_")
+    cold = Cold("pe")
     after = {}
     pour(after, q, [growth(cold, "%[flag]", "%[corr]")] + exp_stream(FS_S1, FS_P1))
     before = {q: list(pending(cold, "%[flag]", "%[corr]", n_o, NOP_AFTER)) + ["s_nop 1"]}
-    return run(D, mf, before, after, 0, par, prologue=list(pending(cold, "%[flag]", "%[corr]", n_o, NOP_AFTER)) + max_stream(FS_S1) + ["s_nop 1"]) + \
+    return run(D, mf, before, after, prologue=list(pending(cold, "%[flag]", "%[corr]", n_o, NOP_AFTER)) + max_stream(FS_S1) + ["s_nop 1"]) + \
         [NOP_AFTER] + cold.text()
 
 
@@ -170,36 +185,37 @@ def gen():
         carry = ['[corr] "+v"(st.corr)', '[flag] "+s"(st.flag)']
         kin = [f'[ka{s}] "v"(ka[{s}])' for s in range(ns)] + ['[ab] "v"(ab)'] + [f'[q{s}] "v"(q[{s}])' for s in range(ns)] + ['[qb] "v"(qb)']
         vin = [f'[va{s}] "v"(va[{s}])' for s in range(2 * nt)]
-        cin, par_in = ['[c] "v"(c)'], ['[par] "s"(par)']
+        cin, group_in = ['[c] "v"(c)'], ['[par] "s"(group)']
         k_args = f"const uint32_t (&ka)[{ns}], uint32_t ab"
-        emit("// c0, c1 = logits of keys 0..31 and 32..63 of the tile in K slot par.  ka, ab: the lane's addresses of the row fragments and of the offset\n"
-             "// operands in K slot 0; q, qb: the queries and what they multiply the offsets with\n",
-             f"logits(int par, {k_args}, {q_args}, f32x16& c0, f32x16& c1)", "",
-             base.both_parities("lg", lambda par: run(D, qk(D, 0) + qk(D, 1), {}, {}, par, 0) + [NOP_AFTER]),
-             ['"=&{v[168:183]}"(c0)', '"=&{v[184:199]}"(c1)'], kin + par_in, range(226, 256))
-        emit("// Start of a run of pipelined steps: logits of the tile in K slot par, softmax of its first half.  c: the lane's logit scale * log2(e);\n"
-             "// corr, flag of the state are outputs\n",
-             f"pipe_start(int par, {k_args}, {q_args}, float& m, float& l, float c, PipeState& st)", "",
-             base.both_parities("pb", lambda par: pipe_start(D, par)),
+        v_args = f"const uint32_t (&va)[{2 * nt}]"
+        emit("// c0, c1 = logits of keys 0..31 and 32..63 of a tile.  ka, ab: the lane's addresses of its row fragments and of its offset operands; q, qb: the\n"
+             "// queries and what they multiply the offsets with\n",
+             f"logits({k_args}, {q_args}, f32x16& c0, f32x16& c1)", "", run(D, qk(D, 0) + qk(D, 1), {}, {}) + [NOP_AFTER],
+             ['"=&{v[168:183]}"(c0)', '"=&{v[184:199]}"(c1)'], kin, range(226, 256))
+        emit("// Start of a run of pipelined steps: logits of a tile, softmax of its first half.  c: the lane's logit scale * log2(e); corr, flag of the\n"
+             "// state are outputs\n",
+             f"pipe_start({k_args}, {q_args}, float& m, float& l, float c, PipeState& st)", "", pipe_start(D),
              ml + ['"=&{v[184:199]}"(st.s1)'] + [x.replace("+", "=&") for x in pa] + ['[corr] "=&v"(st.corr)', '[flag] "=&s"(st.flag)'],
-             kin + cin + par_in, list(s0) + list(p1) + rest)
-        for words in (D // 64, D // 32):
-            conv = [f'[{x}{j}] "v"({x}[{j}])' for x in ("kc", "ks", "km", "vc") for j in range(words)] + \
-                [f'[{x}] "v"({x})' for x in ("vs", "vm0", "vm1", "kst", "vst")] + \
-                [f'[{n}] "{c}"({v})' for n, c, v in (("mask", "v", "0x03c003c0u"), ("one", "s", "0x3c003c00u"), ("low", "v", "0x000f000fu"),
-                                                     ("c1024", "s", "0x64006400u"), ("high", "v", "0x00f000f0u"), ("c64", "s", "0x54005400u"))]
-            arr = f"const uint32_t (&%s)[{words}]"
-            emit("// P V of the tile in V slot par, logits of the next one, in the other K slot.  va: the lane's addresses of the column fragments in V slot 0.\n"
-                 f"// Meanwhile {words} code words of K are converted and written to K slot par, and {words} of V to the other V slot: kc, vc the words, ks, km 16 s and\n"
-                 "// -24 s of a K word's group in fp16, vs, vm0, vm1 s, m - 1024 s and m - 64 s of the V words, kst, vst the lane's addresses in slots 0\n",
-                 f"pipe_step(int par, {k_args}, const uint32_t (&va)[{2 * nt}], {q_args}, {state}, float c,\n"
-                 f"                           {arr % 'kc'}, {arr % 'ks'}, {arr % 'km'}, {arr % 'vc'}, float vs, float vm0, float vm1, uint32_t kst, uint32_t vst)",
-                 "  uint64_t flag1;\n", base.both_parities("ps", lambda par: pipe_step(D, words, par)),
-                 base.o_ops(nt) + ml + [sb] + pa + carry + ['[flag1] "=&s"(flag1)'], kin + vin + cin + par_in + conv,
-                 list(s0) + list(p1) + list(range(CONV_R, CONV_R + 4)) + rest)
-        emit("// End of a run: P V of the tile in V slot par\n",
-             f"pipe_end(int par, const uint32_t (&va)[{2 * nt}], {state}, float c)", "", base.both_parities("pe", lambda par: pipe_end(D, par)),
-             base.o_ops(nt) + ml + [sb] + pa + carry, vin + cin + par_in, list(s0) + list(p1) + rest)
+             kin + cin, list(s0) + list(p1) + rest)
+        step_outs = base.o_ops(nt) + ml + [sb] + pa + carry + ['[flag1] "=&s"(flag1)']
+        emit("// P V of a tile, logits of the next one.  va: the lane's addresses of the tile's column fragments; ka, ab: of the next tile's\n",
+             f"pipe_step({k_args}, {v_args}, {q_args}, {state}, float c)", "  uint64_t flag1;\n", pipe_steps(D, 0, 0, 1), step_outs, kin + vin + cin,
+             list(s0) + list(p1) + rest)
+        words = D // 32
+        conv = [f'[{x}{j}] "v"({x}[{j}])' for x in ("kc", "kf", "vc") for j in range(words)] + \
+            [f'[{x}] "v"({x})' for x in ("vs", "vm0", "vm1", "kst", "vst")] + \
+            [f'[{n}] "{c}"({v})' for n, c, v in (("mask", "v", "0x03c003c0u"), ("one", "s", "0x3c003c00u"), ("low", "v", "0x000f000fu"),
+                                                 ("c1024", "s", "0x64006400u"), ("high", "v", "0x00f000f0u"), ("c64", "s", "0x54005400u"))]
+        arr = f"const uint32_t (&%s)[{words}]"
+        emit("// Two steps: P V of the two tiles of V group `group`, logits of the two of K group `group`, which are one tile further on; addresses are those of\n"
+             f"// group 0.  Meanwhile {words} code words of K and of V are converted and written to the other groups: kc, vc the words, kf 16 s and\n"
+             "// -24 s of a K word's group as two fp16 numbers, vs, vm0, vm1 s, m - 1024 s and m - 64 s of the V words, kst, vst the lane's addresses\n",
+             f"pipe_steps(int group, {k_args}, {v_args}, {q_args}, {state}, float c,\n"
+             f"                            {arr % 'kc'}, {arr % 'kf'}, {arr % 'vc'}, float vs, float vm0, float vm1, uint32_t kst, uint32_t vst)",
+             "  uint64_t flag1;\n", base.both_parities("ps", lambda group: pipe_steps(D, words, group, 2)), step_outs, kin + vin + cin + group_in + conv,
+             list(s0) + list(p1) + list(range(CONV_R, CONV_R + 4)) + rest)
+        emit("// End of a run: P V of the last tile\n", f"pipe_end({v_args}, {state}, float c)", "", pipe_end(D), base.o_ops(nt) + ml + [sb] + pa + carry,
+             vin + cin, list(s0) + list(p1) + rest)
     out.append("}  // namespace cache_pipes\n")
     return "".join(out)
 

@@ -778,10 +778,10 @@ int cache_rows_params(const void* k, const void* v, const pasa_shape_t* shape, c
   return PASA_OK;
 }
 // the rows of a key/value head's query heads are numbered in 32 bits, with room for a last incomplete workgroup and for the splits, and so are
-// the runs of 128 of them of all sequences
+// the runs of 256 of them of all sequences
 bool cache_rows_fit(const pasa_shape_t* s, const pasa_cache_t* c) {
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
-  return rows <= ((int64_t)1 << 30) && s->B * ((rows + 127) / 128) < ((int64_t)1 << 31) - 1024;
+  return rows <= ((int64_t)1 << 30) && s->B * ((rows + 255) / 256) < ((int64_t)1 << 31) - 1024;
 }
 
 // How the rows and tokens of a call are divided among workgroups, and the workspace that takes
@@ -793,7 +793,7 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   CacheAttnPlan a{};
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
-  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 32 ? 16 : rows <= 128 ? 128 : 256;
+  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 32 ? 16 : 256;
   a.splits = 1;
   size_t parts = 0;
   if (a.wg_rows <= 16) {
@@ -801,7 +801,7 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
     while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= 768 && tokens >= (a.splits + 1) * 512) ++a.splits;
     if (a.splits > 1) parts = (size_t)s->B * s->H * s->n * a.splits;
   } else {
-    a.pieces = a.wg_rows == 128 ? 512 : 256;  // as many as can be resident on 256 compute units
+    a.pieces = 256;  // one for every compute unit
     a.row_tiles = (int)((rows + a.wg_rows - 1) / a.wg_rows);
     parts = (size_t)2 * a.pieces * a.wg_rows;
   }

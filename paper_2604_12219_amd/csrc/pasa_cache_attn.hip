@@ -423,7 +423,7 @@ hipError_t launch_rows(const CacheAttnParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream) {
-  if (p.wg_rows >= 128) return pasa_launch_cache_tiles(p, stream);
+  if (p.wg_rows == 256) return pasa_launch_cache_tiles(p, stream);
   const hipError_t rc = launch_rows(p, stream);
   if (rc != hipSuccess || p.splits == 1) return rc;
   const dim3 grid(p.n, p.H, p.c.B);

@@ -34,16 +34,16 @@ struct CacheAttnParams {
   int64_t stride_b, stride_h, stride_n;
   int32_t H, n, causal;
   float scale;  // of the logits, times log2(e)
-  int32_t wg_rows;  // (row, head of a key/value head's share) pairs of a workgroup: 4, 8, 16 (pasa_cache_attn.hip), 128 or 256 (pasa_cache_tile.hip)
+  int32_t wg_rows;  // (row, head of a key/value head's share) pairs of a workgroup: 4, 8, 16 (pasa_cache_attn.hip) or 256 (pasa_cache_tile.hip)
   // 4, 8, 16: a sequence's tokens are divided among `splits` workgroups, at most kCacheMaxSplits, and with splits > 1
   int32_t splits;
   float* part_o;   // fp32 [B][H][n][splits][d]: sums against the maximum of their split
   float* part_ml;  // fp32 [B][H][n][splits][2]: that maximum (log2 units) and the sum of the weights
-  // 128, 256: all the work is divided among `pieces` workgroups; part_o, part_ml are [2 pieces][wg_rows][d], [..][2]
+  // 256: all the work is divided among `pieces` workgroups; part_o, part_ml are [2 pieces][wg_rows][d], [..][2]
   int32_t pieces, row_tiles;  // row_tiles = runs of wg_rows rows that a sequence can have
   CacheMerge* merge;          // [pieces]
 };
 constexpr int kCacheMinPiece = 8;  // tiles: less is not worth sharing an item
 constexpr int kCacheMaxSplits = 64;  // a wave of the merging kernel holds one per lane
-hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // wg_rows 128 or 256
+hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // wg_rows 256
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);

@@ -44,10 +44,10 @@ PASA_DEVICE uint4 values8(uint32_t x, float s, float b0, float b1) {
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// 8 keys' values s (c - 8) of a word of codes in fp16, in the order 0 4 1 5 2 6 3 7; a = 16 s, b = -24 s in fp16
-PASA_DEVICE uint4 keys8(uint32_t x, uint32_t a1, uint32_t b1) {
-  const f16x2 a = __builtin_shufflevector(__builtin_bit_cast(f16x2, a1), __builtin_bit_cast(f16x2, a1), 0, 0);
-  const f16x2 b = __builtin_shufflevector(__builtin_bit_cast(f16x2, b1), __builtin_bit_cast(f16x2, b1), 0, 0);
+// 8 keys' values s (c - 8) of a word of codes in fp16, in the order 0 4 1 5 2 6 3 7; f = (16 s, -24 s)
+PASA_DEVICE uint4 keys8(uint32_t x, uint32_t f) {
+  const f16x2 a = __builtin_shufflevector(__builtin_bit_cast(f16x2, f), __builtin_bit_cast(f16x2, f), 0, 0);
+  const f16x2 b = __builtin_shufflevector(__builtin_bit_cast(f16x2, f), __builtin_bit_cast(f16x2, f), 1, 1);
   const uint32_t h[4] = {((x << 6) & 0x03c003c0u) | 0x3c003c00u, ((x << 2) & 0x03c003c0u) | 0x3c003c00u, ((x >> 2) & 0x03c003c0u) | 0x3c003c00u,
                          ((x >> 6) & 0x03c003c0u) | 0x3c003c00u};
   uint32_t r[4];
@@ -72,88 +72,83 @@ PASA_DEVICE void load_words(const uint8_t* base, uint32_t off, uint32_t (&w)[N])
 
 PASA_DEVICE bool finite_param(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
 
-// A thread's share of a tile: N code words of one token's K, and as many of its V, with the parameters they need.
-// `part` counts the threads of a token: they divide each quarter (the words of one q) of the K codes, and the V codes in order.
-// The tokens of a wave are 8 or 16 consecutive ones, all in one page: what depends on the page is scalar, the lane's offsets stay the same.
-template <int D, int G, int N>
-struct Share {
+// What a thread converts of a group of 128 tokens: the quarter q of one token's K (its code words q * (d/32) ..) and a quarter of its V, with
+// the parameters they need.  The 16 tokens of a wave lie in one page, so what depends on the page is scalar and the lane's offsets stay the same.
+template <int D, int G>
+struct Quarter {
   typedef CacheLayout<D, G> L;
-  static constexpr int PARTS = D / 8 / N, PER_Q = D / 32 / N;  // threads of a token, of a quarter
-  static constexpr int TOKENS = 64 / PARTS;                    // tokens of a wave
-  static constexpr int KG = N * 32 > G ? N * 32 / G : 1;       // groups of a thread's K words
-  static_assert(16 % TOKENS == 0, "");
-  static __device__ constexpr int k_group(int j) { return j * 32 / G; }  // of the j-th word, among them
-  static PASA_DEVICE int quarter(int part) { return part / PER_Q; }
-  static PASA_DEVICE int first_word(int part) { return part % PER_Q * N; }  // in its quarter
-};
-template <int D, int G, int N>
-struct KeyShare : Share<D, G, N> {
-  typedef Share<D, G, N> S;
-  typedef typename S::L L;
-  uint32_t code[N], par[S::KG], bias;  // bias: the parameter of group `quarter`
+  static constexpr int N = D / 32;  // code words of K, and of V
+  // The lane's tokens among the wave's 16: 4 lanes a token.  16 neighbouring lanes write 16-byte chunks of 4 tokens at a time; K's (chunk 4 j + q of a row)
+  // fall into different banks for 4 tokens in a row, V's (chunk (d/32) q + j) for 4 tokens that differ in the two bits which the LDS layout puts
+  // into the low bits of a chunk's place (lds_chunk_off): a four-way conflict otherwise, 450 cycles a tile.
+  static PASA_DEVICE int k_token(int lane) { return lane >> 2; }
+  static PASA_DEVICE int v_token(int lane) {
+    const int t = lane >> 2;
+    return D == 128 ? ((t & 3) << 2) | (t >> 2) : (t & 1) | ((t & 2) << 1) | ((t & 4) >> 1) | (t & 8);
+  }
   struct Offsets {
-    uint32_t code, par, bias;
-    PASA_DEVICE void init(int token, int part) {
-      code = token * L::CODE + 4 * (S::quarter(part) * (D / 32) + S::first_word(part));
-      par = token * L::PARAM + 4 * (S::first_word(part) * 32 / G);
-      bias = token * L::PARAM + 4 * min(S::quarter(part), L::NG - 1);
+    uint32_t k_code, k_par, v_code, v_par;
+    PASA_DEVICE void init(int lane) {
+      const int q = lane & 3, kt = k_token(lane), vt = v_token(lane);
+      k_code = kt * L::CODE + 4 * N * q;
+      k_par = kt * L::PARAM;
+      v_code = vt * L::CODE + 4 * N * q;
+      v_par = vt * L::PARAM + 4 * (8 * N * q / G);
     }
   };
-  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, const Offsets& at) {  // run, slot: of the wave's first token
-    load_words<N>(run + (L::k_codes(page) + slot * L::CODE), at.code, code);
-    load_words<S::KG>(run + (L::k_params(page) + slot * L::PARAM), at.par, par);
-    uint32_t w[1];
-    load_words<1>(run + (L::k_params(page) + slot * L::PARAM), at.bias, w);
-    bias = w[0];
+  uint32_t k_code[N], k_par[L::NG], v_code[N], v_par;
+  // run, slot: page and slot of the wave's first token.  (The offsets are hidden from the compiler, or else it adds them to the page's address
+  // as 64-bit numbers on the vector unit, instead of using the instruction's scalar base.)
+  PASA_DEVICE void load_k(const uint8_t* run, uint32_t page, uint32_t slot, const Offsets& at) {
+    uint32_t code = at.k_code, par = at.k_par;
+    asm("" : "+v"(code), "+v"(par));
+    load_words<N>(run + (L::k_codes(page) + slot * L::CODE), code, k_code);
+    load_words<L::NG>(run + (L::k_params(page) + slot * L::PARAM), par, k_par);
   }
-  // The token's offset operands, 4 fp16 numbers a quarter: (hi, hi, lo, 0) of m + 8 s of group `quarter`, to be multiplied with (hi, lo, hi, 0) of
-  // the group's sum of q
-  PASA_DEVICE uint2 offsets(int part) const {
-    const int quarter = S::quarter(part);
-    const float mid = fmaf(8.f, bf16_low(bias), bf16_high(bias));
+  PASA_DEVICE void load_v(const uint8_t* run, uint32_t page, uint32_t slot, const Offsets& at) {
+    uint32_t code = at.v_code, par = at.v_par, w[1];
+    asm("" : "+v"(code), "+v"(par));
+    load_words<N>(run + (L::v_codes(page) + slot * L::CODE), code, v_code);
+    load_words<1>(run + (L::v_params(page) + slot * L::PARAM), par, w);
+    v_par = w[0];
+  }
+};
+// the same, taken for conversion
+template <int D, int G>
+struct Taken {
+  typedef CacheLayout<D, G> L;
+  static constexpr int N = D / 32;
+  uint32_t kc[N], kf[N], vc[N], v_par;  // kf: 16 s and -24 s of a K word's group in fp16
+  float vs, vm0, vm1;                   // s, m - 1024 s, m - 64 s of the V words' group
+  uint2 bias;  // the token's offset operands of group q: (hi, hi, lo, 0) of m + 8 s, to be multiplied with (hi, lo, hi, 0) of the group's sum of q
+  PASA_DEVICE void take_k(const Quarter<D, G>& x, int q) {
+    uint32_t own = x.k_par[0];
+#pragma unroll
+    for (int g = 1; g < L::NG; ++g) own = q == g ? x.k_par[g] : own;
+    const float mid = fmaf(8.f, bf16_low(own), bf16_high(own));
     const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
     const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
-    uint2 x = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
-    if (quarter >= L::NG) x = make_uint2(0u, 0u);
-    return x;
-  }
-  // 16 s and -24 s of every word's group as fp16 numbers, in the low halves
-  PASA_DEVICE void factors(uint32_t (&a)[N], uint32_t (&b)[N]) const {
+    bias = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+    if (q >= L::NG) bias = make_uint2(0u, 0u);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float s = bf16_low(par[S::k_group(j)]);
-      const f16x2 a2 = {(_Float16)(16.f * s), (_Float16)0.f}, b2 = {(_Float16)(-24.f * s), (_Float16)0.f};
-      a[j] = __builtin_bit_cast(uint32_t, a2);
-      b[j] = __builtin_bit_cast(uint32_t, b2);
+      const float s = bf16_low(x.k_par[j * 32 / G]);
+      const f16x2 f = {(_Float16)(16.f * s), (_Float16)(-24.f * s)};
+      kf[j] = __builtin_bit_cast(uint32_t, f);
+      kc[j] = x.k_code[j];
     }
   }
-  static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, 4 * (S::first_word(part) + j) + S::quarter(part)); }
-};
-template <int D, int G, int N>
-struct ValueShare : Share<D, G, N> {
-  typedef Share<D, G, N> S;
-  typedef typename S::L L;
-  uint32_t code[N], par;
-  struct Offsets {
-    uint32_t code, par;
-    PASA_DEVICE void init(int token, int part) {
-      code = token * L::CODE + 4 * N * part;
-      par = token * L::PARAM + 4 * (8 * N * part / G);
-    }
-  };
-  PASA_DEVICE void load(const uint8_t* run, uint32_t page, uint32_t slot, const Offsets& at) {
-    load_words<N>(run + (L::v_codes(page) + slot * L::CODE), at.code, code);
-    uint32_t w[1];
-    load_words<1>(run + (L::v_params(page) + slot * L::PARAM), at.par, w);
-    par = w[0];
+  PASA_DEVICE void factors(uint32_t par) {
+    vs = bf16_low(par);
+    vm0 = fmaf(-1024.f, vs, bf16_high(par));
+    vm1 = fmaf(-64.f, vs, bf16_high(par));
   }
-  // what values8 takes: s, m - 1024 s, m - 64 s
-  static PASA_DEVICE void factors(uint32_t par, float& s, float& b0, float& b1) {
-    s = bf16_low(par);
-    b0 = fmaf(-1024.f, s, bf16_high(par));
-    b1 = fmaf(-64.f, s, bf16_high(par));
+  PASA_DEVICE void take_v(const Quarter<D, G>& x) {
+    v_par = x.v_par;
+    factors(v_par);
+#pragma unroll
+    for (int j = 0; j < N; ++j) vc[j] = x.v_code[j];
   }
-  static PASA_DEVICE int lds_offset(int token, int part, int j) { return lds_chunk_off<D>(token, N * part + j); }
 };
 
 // ---- who does what ----
@@ -203,15 +198,16 @@ PASA_DEVICE int64_t wave_inclusive_sum(int64_t x, int lane) {
   return x;
 }
 
-template <int D, int G, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnParams p) {
+constexpr int kTileWaves = 8, kTileRows = 32 * kTileWaves;
+
+template <int D, int G>
+__global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAttnParams p) {
   typedef CacheLayout<D, G> L;
-  constexpr int ROWS = WAVES * 32, TILE = 64 * 2 * D;
-  constexpr int N = D / WAVES / 8;  // code words of K, and of V, that a thread converts
-  typedef Share<D, G, N> S;
-  constexpr int BIAS = 64 * 32;
-  __shared__ float bad[2][64];  // of a tile that not every row sees whole: NaN for a token that has values which are not finite, 0 for others
-  __shared__ __attribute__((aligned(1024))) char ring[4 * TILE + 2 * BIAS];  // K, V of one tile, K, V of the next; offset operands of either
+  constexpr int WAVES = kTileWaves, ROWS = kTileRows, TILE = 64 * 2 * D, GROUP = 2 * TILE, BIAS = 64 * 32;
+  // Two groups of two tiles (128 tokens) of K, two of V, the offset operands of K's tokens.  V group v holds the tiles 2 v and 2 v + 1, K group v the
+  // tiles 2 v + 1 and 2 v + 2 (counted from the workgroup's first one): the logits are a tile ahead.  Group v lies in half v & 1.
+  __shared__ __attribute__((aligned(1024))) char ring[4 * GROUP + 4 * BIAS];
+  __shared__ float bad[2][128];  // of V tokens that not every row sees: NaN for a token that has values which are not finite, 0 for others
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
 
   // ---- this workgroup's piece ----
@@ -322,28 +318,26 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
   float m = -INFINITY, l = 0.f;
 
   const uint32_t ring_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
-  // the lane's addresses of the operand fetches in the first K and V slot
+  // the lane's addresses of the operand fetches in the first K tile, its offset operands and the first V tile
   uint32_t ka[D / 16], va[2 * (D / 32)];
-  const uint32_t ab = ring_base + (uint32_t)(4 * TILE + ql * 32 + h * 16);
+  const uint32_t ab = ring_base + (uint32_t)(4 * GROUP + ql * 32 + h * 16);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) ka[s] = (ring_base + (uint32_t)lds_chunk_off<D>(ql, h)) ^ (uint32_t)(s << 5);
   {
     const int i = lane & 15, r = 4 * h + (i >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (i & 3);
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) {
-      va[2 * t] = (ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r, c >> 3) + (c & 7) * 2)) ^ (uint32_t)(t << 6);
-      va[2 * t + 1] = (ring_base + (uint32_t)(TILE + lds_chunk_off<D>(r + 8, c >> 3) + (c & 7) * 2)) ^ (uint32_t)(t << 6);
+      va[2 * t] = (ring_base + (uint32_t)(2 * GROUP + lds_chunk_off<D>(r, c >> 3) + (c & 7) * 2)) ^ (uint32_t)(t << 6);
+      va[2 * t + 1] = (ring_base + (uint32_t)(2 * GROUP + lds_chunk_off<D>(r + 8, c >> 3) + (c & 7) * 2)) ^ (uint32_t)(t << 6);
     }
   }
 
-  // ---- how a tile gets into LDS ----
-  const int token0 = wave * S::TOKENS, token = token0 + lane / S::PARTS, part = tid % S::PARTS;
-  KeyShare<D, G, N> kt;
-  ValueShare<D, G, N> vt;
-  typename KeyShare<D, G, N>::Offsets k_at;
-  typename ValueShare<D, G, N>::Offsets v_at;
-  k_at.init(lane / S::PARTS, part);
-  v_at.init(lane / S::PARTS, part);
+  // ---- how tiles get into LDS ----
+  typedef Quarter<D, G> Raw;
+  const int token0 = wave * 16, quarter = lane & 3, k_token = token0 + Raw::k_token(lane), v_token = token0 + Raw::v_token(lane);  // of a group
+  Raw raw;
+  typename Raw::Offsets raw_at;
+  raw_at.init(lane);
   auto is_page = [&](int pg) -> bool { return pg >= 0 && pg < p.c.n_pages; };
   // Whether all pages of the workgroup's tokens are followed (or else every tile is masked: `followed` below looks each of them up)
   bool pages_good = true;
@@ -359,83 +353,87 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
     return bits;
   };
   const int t_whole = pages_good ? max(min(limit_all >> 6, t_end), t_begin) : t_begin;  // before it every row sees every token
-  // The page of a wave's tokens is looked up a step before their codes are requested, these a step before they are converted.  (Behind the last
-  // tile: some tokens of the sequence, converted and not used)
+  // The page of a wave's tokens is looked up a step (of two tiles) before their codes are requested, these a step before they are converted.
+  // (Before the first and behind the last tile: some tokens of the sequence, converted and not used)
   const int64_t pool_page = (int64_t)p.c.H_kv * p.c.head_bytes;
   const uint8_t* const pool_head = p.c.pool + (int64_t)hkv * p.c.head_bytes;
-  auto look_up = [&](int tile) -> int { return table[min(64 * tile + token0, seq.length - 1) >> p.c.log_page]; };
+  auto k_pos = [&](int v) -> int { return 64 * (t_begin + 2 * v + 1) + token0; };  // first of the wave's tokens of K group v
+  auto v_pos = [&](int v) -> int { return 64 * (t_begin + 2 * v) + token0; };
+  auto look_up = [&](int pos) -> int { return table[min(max(pos, 0), seq.length - 1) >> p.c.log_page]; };
   auto run_of = [&](int pg) -> const uint8_t* { return pool_head + (is_page(pg) ? pg : 0) * pool_page; };
-  auto slot_of = [&](int tile) -> uint32_t { return (uint32_t)(64 * tile + token0) & (page - 1u); };
-  const uint8_t *k_run, *v_run;  // of the tiles to be requested next
-  int next_page;                 // of the tile after k_run's
-  // What a step converts: K of the tile two further down, V of the next one
-  struct {
-    uint32_t kc[N], ks[N], km[N], vc[N], v_par;
-    float vs, vm0, vm1;
-    uint2 bias;
-  } cv;
-  auto take_k = [&](const KeyShare<D, G, N>& share) {
-    share.factors(cv.ks, cv.km);
-    cv.bias = share.offsets(part);
-#pragma unroll
-    for (int j = 0; j < N; ++j) cv.kc[j] = share.code[j];
+  auto slot_of = [&](int pos) -> uint32_t { return (uint32_t)pos & (page - 1u); };
+  int k_page, v_page;  // of the groups to be requested next
+  Taken<D, G> cv;
+  auto request = [&](int v) {  // groups v, whose pages have been looked up
+    raw.load_k(run_of(k_page), page, slot_of(k_pos(v)), raw_at);
+    raw.load_v(run_of(v_page), page, slot_of(v_pos(v)), raw_at);
+    k_page = look_up(k_pos(v + 1));
+    v_page = look_up(v_pos(v + 1));
   };
-  auto take_v = [&]() {
-    cv.v_par = vt.par;
-    vt.factors(vt.par, cv.vs, cv.vm0, cv.vm1);
-#pragma unroll
-    for (int j = 0; j < N; ++j) cv.vc[j] = vt.code[j];
+  auto take = [&](int v) {  // the groups v, which have been requested; the ones after them are
+    cv.take_k(raw, quarter);
+    cv.take_v(raw);
+    request(v + 1);
   };
-  auto take = [&](int t) {  // for the step of tile t; what comes after that is requested
-    take_k(kt);
-    take_v();
-    kt.load(k_run, page, slot_of(t + 3), k_at);
-    vt.load(v_run, page, slot_of(t + 2), v_at);
-    v_run = k_run;
-    k_run = run_of(next_page);
-    next_page = look_up(t + 5);
+  auto store_bias = [&](int v) {
+    *reinterpret_cast<uint2*>(ring + 4 * GROUP + (v & 1) * 2 * BIAS + k_token * 32 + quarter * 8) = cv.bias;
   };
-  auto store_bias = [&](int par) { *reinterpret_cast<uint2*>(ring + 4 * TILE + par * BIAS + token * 32 + S::quarter(part) * 8) = cv.bias; };
-  auto store_k = [&](int par) {
-    store_bias(par);
+  auto store_k = [&](int v) {
+    store_bias(v);
 #pragma unroll
-    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(ring + par * 2 * TILE + kt.lds_offset(token, part, j)) = keys8(cv.kc[j], cv.ks[j], cv.km[j]);
+    for (int j = 0; j < D / 32; ++j)
+      *reinterpret_cast<uint4*>(ring + (v & 1) * GROUP + lds_chunk_off<D>(k_token, 4 * j + quarter)) = keys8(cv.kc[j], cv.kf[j]);
   };
   // Weights of zero do not hide values that are not finite from the rows that do not see them: in a tile that is not whole such values
   // become zeros, and `bad` says so to the rows that do see the token (which are NaN throughout then, not only in the channels of that group)
-  auto store_v = [&](int tile, int par) {
-    if (tile >= t_whole) {
+  auto store_v = [&](int v) {
+    if (t_begin + 2 * v + 2 > t_whole) {
+      const int pos = v_pos(v) + Raw::v_token(lane);
       const bool finite = finite_param(cv.v_par);
-      const bool hide = !finite || 64 * tile + token >= limit_any || (!pages_good && !is_page(look_up(tile)));
-      const uint64_t not_finite = __builtin_amdgcn_ballot_w64(!finite) >> (lane & ~(S::PARTS - 1));
-      if (part == 0) bad[par][token] = (not_finite & ((1u << S::PARTS) - 1u)) ? NAN : 0.f;
-      if (hide) vt.factors(0u, cv.vs, cv.vm0, cv.vm1);
+      const bool hide = pos >= 64 * t_whole && (!finite || pos >= limit_any || (!pages_good && !is_page(look_up(v_pos(v)))));
+      const uint64_t not_finite = __builtin_amdgcn_ballot_w64(!finite) >> (lane & 60);
+      if (quarter == 0) bad[v & 1][v_token] = (not_finite & 15u) ? NAN : 0.f;
+      if (hide) cv.factors(0u);
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      *reinterpret_cast<uint4*>(ring + par * 2 * TILE + TILE + vt.lds_offset(token, part, j)) = values8(cv.vc[j], cv.vs, cv.vm0, cv.vm1);
-  };
-  auto store = [&](int t, int par) {  // what was taken for tile t, which is in the slots par
-    store_k(par);
-    store_v(t + 1, par ^ 1);
+    for (int j = 0; j < D / 32; ++j)
+      *reinterpret_cast<uint4*>(ring + 2 * GROUP + (v & 1) * GROUP + lds_chunk_off<D>(v_token, D / 32 * quarter + j)) = values8(cv.vc[j], cv.vs, cv.vm0, cv.vm1);
   };
   auto meet = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-  // ---- a tile of which not every row sees every token ----
-  auto masked_tile = [&](int tile, int par) {
+  // the addresses for tile x of the four in the ring
+  struct At {
+    uint32_t ka[D / 16], ab, va[2 * (D / 32)];
+  };
+  auto k_at = [&](At& at, int x) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) at.ka[s] = ka[s] + (uint32_t)(x * TILE);
+    at.ab = ab + (uint32_t)(x * BIAS);
+  };
+  auto v_at = [&](At& at, int x) {
+#pragma unroll
+    for (int t = 0; t < 2 * (D / 32); ++t) at.va[t] = va[t] + (uint32_t)(x * TILE);
+  };
+
+  // ---- a tile of which not every row sees every token; k, v: where its K and V are ----
+  auto masked_tile = [&](int tile, int k, int v) {
+    At at;
+    k_at(at, k);
+    v_at(at, v);
     f32x16 s0, s1;
     bf16x8 pf[4];
-    cache_pipes::logits(par, ka, ab, qf, qb, s0, s1);
+    cache_pipes::logits(at.ka, at.ab, qf, qb, s0, s1);
     const int rel = limit - 64 * tile - 4 * h;
     const uint32_t bits = followed(tile);
     int lim[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) lim[t] = (bits >> t) & 1u ? rel : -64;
+    const float* const add = bad[v >> 1] + 64 * (v & 1) + 4 * h;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int key = mfma_row(r, 0);
-      s0[r] += bad[par][key + 4 * h];
-      s1[r] += bad[par][key + 32 + 4 * h];
+      s0[r] += add[key];
+      s1[r] += add[key + 32];
       if (key >= lim[r >> 3]) s0[r] = -INFINITY;
       if (key + 32 >= lim[2 + (r >> 3)]) s1[r] = -INFINITY;
     }
@@ -469,67 +467,90 @@ __global__ void __launch_bounds__(WAVES * 64, 2) cache_tile_kernel(CacheAttnPara
       pf[2][i] = (__bf16)s1[i];
       pf[3][i] = (__bf16)s1[8 + i];
     }
-    const uint32_t off = (uint32_t)(par * 2 * TILE);
-    pipes::cols_x_p64(va[0] + off, va[1] + off, pf, o);
+    pipes::cols_x_p64(at.va[0], at.va[1], pf, o);
   };
 
   if (t_begin < t_end) {
-    // K of the first two tiles and V of the first
-    {
-      KeyShare<D, G, N> k0;
-      const uint8_t* const run0 = run_of(look_up(t_begin));
-      const uint8_t* const run1 = run_of(look_up(t_begin + 1));
-      const uint8_t* const run2 = run_of(look_up(t_begin + 2));
-      k0.load(run0, page, slot_of(t_begin), k_at);
-      vt.load(run0, page, slot_of(t_begin), v_at);
-      kt.load(run1, page, slot_of(t_begin + 1), k_at);
-      take_k(k0);
-      store_k(0);
-      take_k(kt);
-      store_k(1);
-      take_v();
-      store_v(t_begin, 0);
-      vt.load(run1, page, slot_of(t_begin + 1), v_at);
-      kt.load(run2, page, slot_of(t_begin + 2), k_at);
-      v_run = run2;
-      k_run = run_of(look_up(t_begin + 3));
-      next_page = look_up(t_begin + 4);
-    }
+    // K groups -1 (for the first tile) and 0, V group 0; groups 1 requested
+    k_page = look_up(k_pos(-1));
+    raw.load_k(run_of(k_page), page, slot_of(k_pos(-1)), raw_at);
+    k_page = look_up(k_pos(0));
+    v_page = look_up(v_pos(0));
+    cv.take_k(raw, quarter);
+    request(0);
+    store_k(-1);
+    take(0);
+    store_k(0);
+    store_v(0);
     meet();
-    // Before every tile its K and V and the K of the one after it are in LDS.  Whole tiles come first, as a run of pipelined steps, each with
-    // P V of one tile and the logits of the next.
-    int tile = t_begin, par = 0;
+    int tile = t_begin, v = 0;  // V group v and K groups v - 1 and v are in LDS, groups v + 1 requested
     if (tile < t_whole) {
+      // a run of whole tiles in pipelined steps, each with P V of one tile and the logits of the next, two steps between meetings
       pipes::PipeState st;
-      const uint32_t kst = ring_base + (uint32_t)kt.lds_offset(token, part, 0), vst = ring_base + (uint32_t)(TILE + vt.lds_offset(token, part, 0));
-      cache_pipes::pipe_start(0, ka, ab, qf, qb, m, l, c_row, st);
-      meet();  // the first K may be overwritten
+      At at;
+      k_at(at, 3);  // tile 0 is the second one of K group -1
+      cache_pipes::pipe_start(at.ka, at.ab, qf, qb, m, l, c_row, st);
+      meet();  // K group -1 may be overwritten
+      const uint32_t kst = ring_base + (uint32_t)lds_chunk_off<D>(k_token, quarter), vst = ring_base + (uint32_t)(2 * GROUP + lds_chunk_off<D>(v_token, D / 32 * quarter));
 #pragma unroll 1
-      for (; tile < t_whole - 1; ++tile) {
-        take(tile);
-        store_bias(par);
+      for (; tile + 3 < t_whole; tile += 2) {
+        take(v + 1);
+        store_bias(v + 1);
         // the conversion runs in the shadow of the matrix instructions
-        cache_pipes::pipe_step(par, ka, ab, va, qf, qb, o, m, l, st, c_row, cv.kc, cv.ks, cv.km, cv.vc, cv.vs, cv.vm0, cv.vm1, kst, vst);
-        par ^= 1;
+        cache_pipes::pipe_steps(v & 1, ka, ab, va, qf, qb, o, m, l, st, c_row, cv.kc, cv.kf, cv.vc, cv.vs, cv.vm0, cv.vm1, kst, vst);
+        ++v;
         meet();
       }
-      take(tile);
-      store(tile, par);
-      cache_pipes::pipe_end(par, va, o, m, l, st, c_row);
+      const bool three = tile + 2 < t_whole;  // whole tiles that are left (or one or two): the next V group holds one that is not whole, or is none
+      if (three) {
+        take(v + 1);
+        store_k(v + 1);
+        store_v(v + 1);
+      }
+#pragma unroll 1
+      for (int x = 0; x < 2 && tile + 1 < t_whole; ++x, ++tile) {
+        k_at(at, 2 * (v & 1) + x);
+        v_at(at, 2 * (v & 1) + x);
+        cache_pipes::pipe_step(at.ka, at.ab, at.va, qf, qb, o, m, l, st, c_row);
+      }
+      if (three) {
+        ++v;
+        meet();
+      }
+      v_at(at, 2 * (v & 1) + ((tile - t_begin) & 1));
+      cache_pipes::pipe_end(at.va, o, m, l, st, c_row);
       ++tile;
-      par ^= 1;
-      meet();
+      if (((tile - t_begin) & 1) == 0 && tile < t_end) {  // V group v is used up
+        take(v + 1);
+        meet();
+        store_k(v + 1);
+        store_v(v + 1);
+        ++v;
+        meet();
+      }
     }
 #pragma unroll 1
-    for (; tile < t_end; ++tile) {
-      masked_tile(tile, par);
-      meet();
-      take(tile);
-      store(tile, par);
-      par ^= 1;
-      meet();
+    while (tile < t_end) {
+      // the two tiles of V group v: their K is the second one of K group v - 1 and the first one of K group v
+      if (((tile - t_begin) & 1) == 0) {
+        masked_tile(tile, 2 * ((v - 1) & 1) + 1, 2 * (v & 1));
+        ++tile;
+      }
+      if (tile < t_end) {
+        masked_tile(tile, 2 * (v & 1), 2 * (v & 1) + 1);
+        ++tile;
+      }
+      if (tile < t_end) {
+        take(v + 1);
+        meet();
+        store_k(v + 1);
+        store_v(v + 1);
+        ++v;
+        meet();
+      }
     }
   }
+  meet();  // the next part's tiles may be written
 
   l = half_swap_sum(l);
   if (row <= last_row) {
@@ -617,8 +638,7 @@ __global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
 
 template <int D, int G>
 hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
-  if (p.wg_rows == 128) cache_tile_kernel<D, G, 4><<<p.pieces, 256, 0, stream>>>(p);
-  else cache_tile_kernel<D, G, 8><<<p.pieces, 512, 0, stream>>>(p);
+  cache_tile_kernel<D, G><<<p.pieces, kTileWaves * 64, 0, stream>>>(p);
   cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 4), 256, 0, stream>>>(p);
   return hipGetLastError();
 }
