@@ -793,16 +793,40 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   CacheAttnPlan a{};
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
-  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 32 ? 16 : 256;
+  // 4, 8 or 16 rows a workgroup (cache_rows_kernel) take time with the runs of 16 rows and the tiles of 64 tokens, 0.0028 us each with groups of 32 of 128
+  // channels, 0.0019 with groups of 64 or 64 channels, 0.0016 with one group of 128; 256 rows (cache_tile_kernel) with the tiles, 0.0088 us, and some
+  // 25 us more before and after them.  us, 16 rows / 256:
+  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 18.1 / 28.0, 500 rows 19.2 / 33.3; 1 head, 200,000 tokens, 33 rows 59 / 115; 40,000, 128 rows
+  //     31.5 / 54.7; 64 heads of 4000, 33 rows 52 / 76, 64 71 / 78, 192 148 / 93; 8 heads of 20,000, 100 rows 79 / 69; 40 heads of 75,600, 40 rows 426 / 438,
+  //     64 594 / 448
+  //   groups of 64: 64 heads of 4000, 33 rows 41 / 74; of 128: 64 rows 46 / 74, 128 66 / 80
+  //   d = 64: 64 heads of 4000, 33 rows 29 / 47, 64 37 / 48, 128 54.3 / 52.5, 200 92 / 56; 40 heads of 75,600, 64 rows 268 / 280
+  const double head_tiles = (double)s->B * c->H_kv * ((tokens + 63) / 64), weight = c->group == 128 ? 2 : s->d == 128 && c->group == 32 ? 4 : 3;
+  a.row_tiles = (int)((rows + 255) / 256);
+  const bool few = weight * head_tiles * ((rows + 15) / 16) <= 32768 + 12 * head_tiles * a.row_tiles;
+  a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : few ? 16 : 256;
   a.splits = 1;
   size_t parts = 0;
   if (a.wg_rows <= 16) {
     const int64_t wgs = (int64_t)s->B * c->H_kv * ((rows + a.wg_rows - 1) / a.wg_rows);
-    while (a.splits < kCacheMaxSplits && wgs * (a.splits + 1) <= 768 && tokens >= (a.splits + 1) * 512) ++a.splits;
+    // The time of a workgroup is its steps (its four waves take a tile each) and some three more before and after them.  The workgroups of one sequence
+    // are alike and go in rounds of those that are resident together; sequences may be of any lengths, so of several the workgroups follow each other
+    // and leave half a workgroup's time at the end.  The merging is worth two steps.  us, by splits: one token of 75,600, 40 heads: 12 99, 19 109, 25
+    // 100, 38 103; 40 rows, 40 heads 4 380, 6 430, 8 368, 12 395; 32 sequences of 800 to 8000 tokens, 8 heads 2 50.5, 3 47.8, 4 47.5, 6 51.5; 64 heads of
+    // 2000 tokens, 33 rows 2 35.6, 3 43
+    const int resident = 256 * (s->d == 64 ? (c->group == 32 && a.wg_rows == 16 ? 3 : 4) : c->group == 32 || (c->group == 64 && a.wg_rows == 16) ? 2 : 3);
+    const int64_t tiles = (tokens + 63) / 64;
+    int64_t best = INT64_MAX;
+    for (int n = 1; n <= kCacheMaxSplits && (n == 1 || tokens >= n * 512); ++n) {
+      const int64_t rounds = (wgs * n + resident - 1) / resident, steps = ((tiles + n - 1) / n + 3) / 4;
+      const int64_t cost = s->B == 1 ? rounds * (steps + 3) * 64 : wgs * n * (steps + 3) * 64 / resident + (steps + 3) * 32;
+      if (cost + (n > 1 ? 128 : 0) < best) { best = cost + (n > 1 ? 128 : 0); a.splits = n; }
+    }
     if (a.splits > 1) parts = (size_t)s->B * s->H * s->n * a.splits;
   } else {
-    a.pieces = 256;  // one for every compute unit
-    a.row_tiles = (int)((rows + a.wg_rows - 1) / a.wg_rows);
+    // one for every compute unit, and if there are fewer than four heads' runs of rows, 64 for each: one head of 40,000 tokens, 40 rows 55 us with 64,
+    // 61 with 32, 66 with 128
+    a.pieces = (int)std::min<int64_t>(256, 64 * (int64_t)s->B * c->H_kv * a.row_tiles);
     parts = (size_t)2 * a.pieces * a.wg_rows;
   }
   a.part_ml = align_up(parts * s->d * 4);

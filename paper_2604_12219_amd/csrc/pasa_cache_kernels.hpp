@@ -43,7 +43,7 @@ struct CacheAttnParams {
   int32_t pieces, row_tiles;  // row_tiles = runs of wg_rows rows that a sequence can have
   CacheMerge* merge;          // [pieces]
 };
-constexpr int kCacheMinPiece = 8;  // tiles: less is not worth sharing an item
+constexpr int kCacheMinPiece = 2;  // tiles of a piece, at least
 constexpr int kCacheMaxSplits = 64;  // a wave of the merging kernel holds one per lane
 hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // wg_rows 256
 hipError_t pasa_launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);

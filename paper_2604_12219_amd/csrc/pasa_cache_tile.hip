@@ -2,8 +2,8 @@
 //
 // Bound by the matrix cores, as attention over bf16 is: tiles of 64 tokens in LDS, and instruction streams over them (pasa_cache_pipes.hpp).
 // What differs is how a tile gets there: a thread holds a few code words of one token, of K and of V, converts them and writes them
-// to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, so the wider one
-// (eight waves, 256 rows) pays half as much a row.
+// to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, hence eight waves
+// and 256 rows: with four waves and 128 it costs twice as much a row.
 //
 //   V: bf16(s c + m).  An and-or (and one shift for half of a word) makes fp16 numbers 1024 + c or 64 + c of two codes, a mixed fma
 //     s c + m of each (s (1024 + c) + (m - 1024 s): the rounding of that is 2^-13 of s), a conversion rounds two of them to bf16: 2.1 instructions a
@@ -22,6 +22,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 typedef __attribute__((address_space(4))) const int32_t const_i32;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // 8 values of a word of codes in bf16; b0 = m - 1024 s, b1 = m - 64 s
 PASA_DEVICE uint4 values8(uint32_t x, float s, float b0, float b1) {
@@ -156,7 +157,7 @@ struct Taken {
 // see (at least one where there are rows: somebody has to write them).  All items of all heads in a row, head by head, are a line of
 // tiles that the workgroups divide evenly, each a piece of `piece` of them: so an item can be shared by several workgroups, and the last ones have no
 // less to do than the first, whatever the lengths are (they are known on the device only).  Against one workgroup an item: 40 heads of 15 items,
-// 600 workgroups on 256 compute units, 7640 -> us.
+// 600 workgroups on 256 compute units, 14,400 rows and 75,600 tokens, 7640 -> 6300 us.
 // A workgroup's piece holds at most two parts of items: one at its start (slot 2 w of the partial results) and one at its end (slot 2 w + 1).
 struct CacheItem {
   int b, row0, rows;  // rows: of the sequence, times the share of heads
@@ -576,10 +577,10 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
       if (h == 0) { p.part_ml[2 * part_row] = m; p.part_ml[2 * part_row + 1] = l; }
     }
   }
-  if (tid == 0 && !whole_item && off + take_tiles == weight) {  // the last part of a shared item: cache_merge_items puts it together
+  if (tid == 0 && off != 0) {  // not the first part of a shared item: cache_merge_items puts it together
     const int64_t start = at - off;
     const int w0 = (int)(start / piece);
-    p.merge[blockIdx.x] = {hkv, item, 2 * w0 + (start % piece != 0 ? 1 : 0), (int)blockIdx.x - w0 + 1};
+    p.merge[blockIdx.x] = {hkv, item, 2 * w0 + (start % piece != 0 ? 1 : 0), (int)((start + weight - 1) / piece) - w0 + 1};
   }
   at += take_tiles;
   off = 0;
@@ -592,54 +593,93 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   }
 }
 
-// Items that several workgroups share, from their parts: workgroup (w, y) handles rows 4 y .. of the item whose last part workgroup w of cache_tile_kernel
-// had, a row a wave.
+// Items that several workgroups share, from their parts.  Its time is a chain of loads, so four rows go side by side: few parts by one wave, its lanes on
+// 64/LANES parts at a time, workgroup (w, y) on rows 16 y .. of the item whose last part workgroup w of cache_tile_kernel had; many parts, of few
+// rows if they are not that many, by the four waves of a workgroup, each a quarter, and by the workgroups (w, y) of all parts but the first.
 template <int D>
 __global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
+  constexpr int LANES = D / 4, PP = 64 / LANES, R = 4, WAVES = 4;  // lanes of a part's row, parts at a time in a wave, rows
+  __shared__ f32x4 s_o[WAVES - 1][R][LANES];
+  __shared__ float s_sum[WAVES - 1][R];
   const CacheMerge mg = p.merge[blockIdx.x];
   if (mg.parts == 0) return;
   const CacheItem it = cache_item(p, mg.item);
-  const int lane = threadIdx.x & 63, share = p.H / p.c.H_kv;
-  const int r = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), row = it.row0 + r;
-  if (row >= it.rows) return;
-  // part 0 in slot first_slot, the others at the starts of the workgroups after that
-  auto place = [&](int j) -> int64_t { return (j == 0 ? mg.first_slot : (int64_t)2 * (mg.first_slot / 2 + j)) * p.wg_rows + r; };
-  float top = -INFINITY;
-  for (int j = lane; j < mg.parts; j += 64) top = fmaxf(top, p.part_ml[2 * place(j)]);
-  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, o[D / 64] = {};
-  for (int j0 = 0; j0 < mg.parts; j0 += 64) {
-    float f = 0.f;
-    if (j0 + lane < mg.parts) {
-      const float* const ml = p.part_ml + 2 * place(j0 + lane);
-      f = __builtin_amdgcn_exp2f(ml[0] - ref);
-      sum = fmaf(f, ml[1], sum);
-    }
-    const int count = min(64, mg.parts - j0);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int part = (int)blockIdx.x - mg.first_slot / 2, last = min((int)(gridDim.y * WAVES * R), it.rows - it.row0) - 1;
+  const bool shared = mg.parts > 2 * PP && last < (mg.parts - 1) * (int)gridDim.y * R;  // by the waves, all rows at once
+  if (!shared && part != mg.parts - 1) return;
+  const int r0 = (shared ? (part - 1) * (int)gridDim.y + (int)blockIdx.y : (int)blockIdx.y * WAVES + wave) * R;
+  if (r0 > last) return;
+  const int share = p.H / p.c.H_kv, sub = lane / LANES, ch = lane % LANES * 4;
+  // part 0 in slot first_slot, the others at the starts of the workgroups after that; rows behind the last one are the last one again, not written
+  auto place = [&](int j, int k) -> int64_t {
+    return (j == 0 ? mg.first_slot : (int64_t)2 * (mg.first_slot / 2 + j)) * p.wg_rows + min(r0 + k, last);
+  };
+  float top[R], sum[R];
+  f32x4 o[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) { top[k] = -INFINITY; sum[k] = 0.f; o[k] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  for (int j = lane; j < mg.parts; j += 64)
+#pragma unroll
+    for (int k = 0; k < R; ++k) top[k] = fmaxf(top[k], p.part_ml[2 * place(j, k)]);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    for (int d = 32; d >= 1; d >>= 1) top[k] = fmaxf(top[k], __shfl_xor(top[k], d));
+    if (top[k] == -INFINITY) top[k] = 0.f;
+  }
 #pragma unroll 4
-    for (int j = 0; j < count; ++j) {
-      const float fj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f), j));
-      const float* const src = p.part_o + place(j0 + j) * D + lane;
+  for (int j = (shared ? wave * PP : 0) + sub; j < mg.parts; j += shared ? WAVES * PP : PP) {
 #pragma unroll
-      for (int t = 0; t < D / 64; ++t) o[t] = fmaf(fj, src[64 * t], o[t]);
+    for (int k = 0; k < R; ++k) {
+      const int64_t at = place(j, k);
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + at * D + ch);
+      const float f = __builtin_amdgcn_exp2f(ml.x - top[k]);
+      sum[k] = fmaf(f, ml.y, sum[k]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[k][i] = fmaf(f, x[i], o[k][i]);
     }
   }
-  for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-  const int i = row / share, h = mg.hkv * share + row % share;
-  uint16_t* const out = p.o + it.b * p.stride_b + h * p.stride_h + i * p.stride_n;
 #pragma unroll
-  for (int t = 0; t < D / 64; ++t) {
-    const __bf16 y = (__bf16)(sum == 0.f ? 0.f : o[t] / sum);
-    out[64 * t + lane] = __builtin_bit_cast(uint16_t, y);
+  for (int k = 0; k < R; ++k) {
+#pragma unroll
+    for (int d = LANES; d < 64; d <<= 1) {
+      sum[k] += __shfl_xor(sum[k], d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[k][i] += __shfl_xor(o[k][i], d);
+    }
+    if (shared && wave > 0 && sub == 0) {
+      s_o[wave - 1][k][lane] = o[k];
+      s_sum[wave - 1][k] = sum[k];
+    }
   }
-  if (p.lse && lane == 0) p.lse[((int64_t)it.b * p.H + h) * p.n + i] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+  if (shared) {
+    __syncthreads();
+    if (wave > 0) return;
+  }
+  if (sub != 0) return;
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (r0 + k > last) break;
+    if (shared)
+#pragma unroll
+      for (int w = 0; w < WAVES - 1; ++w) {
+        o[k] += s_o[w][k][lane];
+        sum[k] += s_sum[w][k];
+      }
+    const int row = it.row0 + r0 + k, i = row / share, h = mg.hkv * share + row % share;
+    const float inv = sum[k] == 0.f ? 0.f : 1.f / sum[k];
+    const bf16x2 x0 = {(__bf16)(o[k][0] * inv), (__bf16)(o[k][1] * inv)}, x1 = {(__bf16)(o[k][2] * inv), (__bf16)(o[k][3] * inv)};
+    *reinterpret_cast<uint2*>(p.o + it.b * p.stride_b + h * p.stride_h + i * p.stride_n + ch) =
+        make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
+    if (p.lse && ch == 0) p.lse[((int64_t)it.b * p.H + h) * p.n + i] = sum[k] == 0.f ? -INFINITY : (top[k] + __builtin_amdgcn_logf(sum[k])) * kLn2;
+  }
 }
 
 template <int D, int G>
 hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
   cache_tile_kernel<D, G><<<p.pieces, kTileWaves * 64, 0, stream>>>(p);
-  cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 4), 256, 0, stream>>>(p);
+  cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 16), 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
