@@ -377,6 +377,8 @@ PASA_API int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cach
 /*
  * O = softmax(Q K^T * scale) V over the cached tokens t < len[b]; with causal != 0 a row sees the tokens up to and including its own
  * only.  shape->H is a multiple of H_kv: head h attends over key/value head h / (H / H_kv).  A row that sees no token is zero, its lse -inf.
+ * A row that sees a token of which a group reads back as NaN is NaN, lse included, if it is a group of K, and NaN in the channels of that
+ * group, perhaps in others, if it is one of V.  Logits are held in binary32: beyond +-2^30 their spacing makes the weights overflow.
  *   q, out  bf16 [B, H, n, d] (shape strides);  lse fp32 [B*H, n] or NULL
  *   n_max   host: what len is expected not to exceed, 0 for max_pages * page.  The work is divided for this length; longer
  *           sequences are computed as well, only more slowly.

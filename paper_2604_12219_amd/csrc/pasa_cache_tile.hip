@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   // Two groups of two tiles (128 tokens) of K, two of V, the offset operands of K's tokens.  V group v holds the tiles 2 v and 2 v + 1, K group v the
   // tiles 2 v + 1 and 2 v + 2 (counted from the workgroup's first one): the logits are a tile ahead.  Group v lies in half v & 1.
   __shared__ __attribute__((aligned(1024))) char ring[4 * GROUP + 4 * BIAS];
-  __shared__ float bad[2][128];  // of V tokens that not every row sees: NaN for a token that has values which are not finite, 0 for others
+  __shared__ bool bad[2][128];  // V tokens that not every row sees: has values that are not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, h = lane >> 5;
 
   // ---- this workgroup's piece ----
@@ -386,14 +386,14 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
       *reinterpret_cast<uint4*>(ring + (v & 1) * GROUP + lds_chunk_off<D>(k_token, 4 * j + quarter)) = keys8(cv.kc[j], cv.kf[j]);
   };
   // Weights of zero do not hide values that are not finite from the rows that do not see them: in a tile that is not whole such values
-  // become zeros, and `bad` says so to the rows that do see the token (which are NaN throughout then, not only in the channels of that group)
+  // become zeros, and `bad` says so to the rows that do see the token (whose outputs are NaN then in all channels, not only in those of that group)
   auto store_v = [&](int v) {
     if (t_begin + 2 * v + 2 > t_whole) {
       const int pos = v_pos(v) + Raw::v_token(lane);
       const bool finite = finite_param(cv.v_par);
       const bool hide = pos >= 64 * t_whole && (!finite || pos >= limit_any || (!pages_good && !is_page(look_up(v_pos(v)))));
       const uint64_t not_finite = __builtin_amdgcn_ballot_w64(!finite) >> (lane & 60);
-      if (quarter == 0) bad[v & 1][v_token] = (not_finite & 15u) ? NAN : 0.f;
+      if (quarter == 0) bad[v & 1][v_token] = (not_finite & 15u) != 0u;
       if (hide) cv.factors(0u);
     }
 #pragma unroll
@@ -429,12 +429,9 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
     int lim[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) lim[t] = (bits >> t) & 1u ? rel : -64;
-    const float* const add = bad[v >> 1] + 64 * (v & 1) + 4 * h;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int key = mfma_row(r, 0);
-      s0[r] += add[key];
-      s1[r] += add[key + 32];
       if (key >= lim[r >> 3]) s0[r] = -INFINITY;
       if (key + 32 >= lim[2 + (r >> 3)]) s1[r] = -INFINITY;
     }
@@ -469,6 +466,18 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
       pf[3][i] = (__bf16)s1[8 + i];
     }
     pipes::cols_x_p64(at.va[0], at.va[1], pf, o);
+    uint64_t not_finite = __builtin_amdgcn_ballot_w64(bad[v >> 1][64 * (v & 1) + lane]);
+    if (not_finite != 0u) {  // hardly ever
+      float add = 0.f;
+      for (; not_finite != 0u; not_finite &= not_finite - 1u) {
+        const int key = __builtin_ctzll(not_finite);
+        if (64 * tile + key < limit && ((bits >> (key >> 4)) & 1u)) add = NAN;
+      }
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] += add;
+    }
   };
 
   if (t_begin < t_end) {
