@@ -35,10 +35,13 @@ typedef __attribute__((address_space(4))) const int32_t const_i32;
 
 PASA_DEVICE f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// a word of 8 codes as 16 + c in bf16, in the order 0 4 1 5 2 6 3 7
-PASA_DEVICE bf16x8 codes_bf16(uint32_t x) {
-  const u32x4 w = {((x << 3) & 0x00780078u) | 0x41804180u, ((x >> 1) & 0x00780078u) | 0x41804180u, ((x >> 5) & 0x00780078u) | 0x41804180u,
-                   ((x >> 9) & 0x00780078u) | 0x41804180u};
+// a word of 8 codes as 16 + c in bf16, in the order 0 4 1 5 2 6 3 7.  The constants come in registers (CodeBits), where an and-or can have them.
+struct CodeBits {
+  uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+  PASA_DEVICE CodeBits() { asm("" : "+s"(mask), "+v"(sixteen)); }
+};
+PASA_DEVICE bf16x8 codes_bf16(uint32_t x, const CodeBits& k) {
+  const u32x4 w = {((x << 3) & k.mask) | k.sixteen, ((x >> 1) & k.mask) | k.sixteen, ((x >> 5) & k.mask) | k.sixteen, ((x >> 9) & k.mask) | k.sixteen};
   return __builtin_bit_cast(bf16x8, w);
 }
 // 8 bf16 in that order
@@ -220,6 +223,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
   const uint8_t* const v_read = vl + v_token * L::CODE;
   const int w_row = (col >> 2) * NR + min(col & 3, NR - 1);  // the row of slot col (or, unused slots, any)
 
+  const CodeBits bits16;
   int tile = split * per + wave;
   if (tile < t_end) {
     find(tile);
@@ -256,7 +260,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
       for (int g = 0; g < NG; ++g) {
         f32x4 acc = start[g];
 #pragma unroll
-        for (int j = g * WPG; j < (g + 1) * WPG; ++j) acc = mfma16(qf[j], codes_bf16(kc[t][j]), acc);
+        for (int j = g * WPG; j < (g + 1) * WPG; ++j) acc = mfma16(qf[j], codes_bf16(kc[t][j], bits16), acc);
         const float sc = bf16_low(kp[t][g]), mn = bf16_high(kp[t][g]) * -0.0625f;  // (times start: the minimum times the sum of q)
 #pragma unroll
         for (int i = 0; i < NR; ++i) s[t][i] = fmaf(sc, acc[i], g == 0 ? mn * start[g][i] : fmaf(mn, start[g][i], s[t][i]));
@@ -265,18 +269,24 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
     }
     load_k();
     __builtin_amdgcn_sched_barrier(0);
+    if (!whole)
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t][i] = key[t] < limit[i] ? s[t][i] : -INFINITY;
+    // The maximum follows the logits only when one is 64 times its weight's due ahead: o and l are as exact with weights up to 64 as with weights up to
+    // 1, and the maximum over the lanes is rarely needed.
     float mx[NR];
     bool grows = false;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) s[t][i] = key[t] < limit[i] ? s[t][i] : -INFINITY;
-      mx[i] = row16_max(fmaxf(fmaxf(s[0][i], s[1][i]), fmaxf(s[2][i], s[3][i]))) * p.scale;
-      grows |= mx[i] > m[i];
+      mx[i] = fmaxf(fmaxf(s[0][i], s[1][i]), fmaxf(s[2][i], s[3][i]));
+      grows |= fmaf(mx[i], p.scale, -m[i]) > 6.f;
     }
     if (__builtin_amdgcn_ballot_w64(grows)) {
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
+        mx[i] = row16_max(mx[i]) * p.scale;
         const float m_new = fmaxf(m[i], mx[i]);
         const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - m_new);
         m[i] = m_new;
@@ -337,8 +347,8 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
 #pragma unroll
       for (int c = g * (G / 16); c < (g + 1) * (G / 16); ++c) {
         const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(v_read + 8 * c));
-        o[c] = mfma16(w0, codes_bf16((uint32_t)v[0]), o[c]);
-        o[c] = mfma16(w1, codes_bf16((uint32_t)v[1]), o[c]);
+        o[c] = mfma16(w0, codes_bf16((uint32_t)v[0], bits16), o[c]);
+        o[c] = mfma16(w1, codes_bf16((uint32_t)v[1], bits16), o[c]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
