@@ -793,17 +793,17 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   CacheAttnPlan a{};
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
-  // 4, 8 or 16 rows a workgroup (cache_rows_kernel) take time with the runs of 16 rows and the tiles of 64 tokens, 0.0028 us each with groups of 32 of 128
-  // channels, 0.0019 with groups of 64 or 64 channels, 0.0016 with one group of 128; 256 rows (cache_tile_kernel) with the tiles, 0.0088 us, and some
-  // 25 us more before and after them.  us, 16 rows / 256:
-  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 18.1 / 28.0, 500 rows 19.2 / 33.3; 1 head, 200,000 tokens, 33 rows 59 / 115; 40,000, 128 rows
-  //     31.5 / 54.7; 64 heads of 4000, 33 rows 52 / 76, 64 71 / 78, 192 148 / 93; 8 heads of 20,000, 100 rows 79 / 69; 40 heads of 75,600, 40 rows 426 / 438,
-  //     64 594 / 448
-  //   groups of 64: 64 heads of 4000, 33 rows 41 / 74; of 128: 64 rows 46 / 74, 128 66 / 80
-  //   d = 64: 64 heads of 4000, 33 rows 29 / 47, 64 37 / 48, 128 54.3 / 52.5, 200 92 / 56; 40 heads of 75,600, 64 rows 268 / 280
+  // 4, 8 or 16 rows a workgroup (cache_rows_kernel) take time with the runs of 16 rows and the tiles of 64 tokens: 0.0024 us each with groups of 32 of
+  // 128 channels, 0.0021 with groups of 64, 0.0013 with one of 128, 0.0012 with 64 channels.  256 rows (cache_tile_kernel) take time with the tiles, 0.0093
+  // us, 0.0058 with 64 channels, and some 28 us more before and after them.  us, 16 rows / 256:
+  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 17.0 / 28.0, 500 rows 18.7 / 34.5; 1 head, 200,000 tokens, 33 rows 55 / 114; 40,000, 128 rows
+  //     31 / 54; 8 heads of 20,000, 100 rows 55 / 68; 64 heads of 4000, 33 rows 50 / 76, 64 55 / 78, 128 84 / 84, 192 133 / 94; 40 heads of 75,600, 40
+  //     rows 350 / 447, 64 472 / 453
+  //   groups of 64: 64 heads of 4000, 33 rows 39 / 74; of 128: 64 rows 40 / 75, 128 57 / 81
+  //   d = 64: 64 heads of 4000, 33 rows 26 / 47, 64 34 / 49, 128 47 / 53, 200 79 / 57; 40 heads of 75,600, 64 rows 220 / 281
   const double head_tiles = (double)s->B * c->H_kv * ((tokens + 63) / 64), weight = c->group == 128 ? 2 : s->d == 128 && c->group == 32 ? 4 : 3;
   a.row_tiles = (int)((rows + 255) / 256);
-  const bool few = weight * head_tiles * ((rows + 15) / 16) <= 32768 + 12 * head_tiles * a.row_tiles;
+  const bool few = weight * head_tiles * ((rows + 15) / 16) <= 49152 + 14 * head_tiles * a.row_tiles;
   a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : few ? 16 : 256;
   a.splits = 1;
   size_t parts = 0;
