@@ -10,10 +10,22 @@ Run `python gen_cache_pipes.py` in this directory after changing it; the header 
 import os
 
 import gen_mfma_pipes as base
-from gen_mfma_pipes import FS_P0, FS_P1, FS_S0, FS_S1, FS_T, MFMA, NOP_AFTER, Cold, F, exp_stream, growth, max_stream, off, pending, pour, vr
+from gen_mfma_pipes import FS_P0, FS_P1, FS_S0, FS_S1, FS_T, MFMA, NOP_AFTER, Cold, F, exp_stream, max_stream, off, pending, pour, vr
 
 MFMA_F16 = "v_mfma_f32_32x32x16_f16"
 BIAS_ROW = 32  # bytes of a key's offset operands
+
+
+def growth(cold, flag, corr):
+    """after max_stream: where the lane's maximum is larger than m, m <- that + 8, and l and the factor `corr` for the accumulators follow; `flag` is not zero
+    then.  m so stands for a bound of the logits that they reach seldom: weights start at 2^-8 instead of 1 (to the same relative accuracy), and of the 64
+    tiles of 4096 tokens a few change m, where an exact maximum makes one of a wave's 32 rows do so in most of them."""
+    t0, t1, t2 = (vr(FS_T + i) for i in range(3))
+    body = [f"v_mov_b32 {t1}, {t0}", "s_nop 1", f"v_permlane32_swap_b32 {t0}, {t1}", "s_nop 0",
+            f"v_max_f32 {t0}, {t0}, {t1}", f"v_add_f32 {t1}, 0x41000000, {t0}", f"v_cmp_gt_f32 vcc, {t0}, %[m]", "s_nop 1",
+            f"v_cndmask_b32 {t1}, %[m], {t1}, vcc", f"v_sub_f32 {t2}, %[m], {t1}", f"v_exp_f32 {corr}, {t2}",
+            f"v_mov_b32 %[m], {t1}", "s_nop 0", f"v_mul_f32 %[l], %[l], {corr}"]
+    return tuple([f"v_cmp_gt_f32 vcc, {t0}, %[m]", f"s_mov_b64 {flag}, vcc"] + cold.block("s_cbranch_vccnz", body))
 
 
 def qk(D, half, tile=0):

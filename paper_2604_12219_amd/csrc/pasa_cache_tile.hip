@@ -270,6 +270,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   const int own = min(row, last_row), i_own = own / share, h_own = hkv * share + own % share;
   const int64_t row_off = b * p.stride_b + h_own * p.stride_h + i_own * p.stride_n;
   const int limit = row_limit(p, seq, own);
+  const int limit_wave = __builtin_amdgcn_readfirstlane(row_limit(p, seq, min(row0 + wave * 32 + 31, last_row)));
   // q / 2^e in fp16, 2^e the power of two at the row's largest magnitude, in the order of a word's codes; qb: the groups' sums of that
   f16x8 qf[D / 16], qb;
   float c_row;  // logit scale times log2(e) times 2^e
@@ -418,6 +419,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
 
   // ---- a tile of which not every row sees every token; k, v: where its K and V are ----
   auto masked_tile = [&](int tile, int k, int v) {
+    if (64 * tile >= limit_wave) return;  // none of the wave's rows sees any of it
     At at;
     k_at(at, k);
     v_at(at, v);
@@ -440,7 +442,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
     for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, s0[r]), s1[r]);
     mx = half_swap_max(mx) * c_row;
     if (__builtin_amdgcn_ballot_w64(mx > m)) {
-      const float m_new = fmaxf(m, mx);
+      const float m_new = mx > m ? mx + 8.f : m;  // (as in the pipelined steps)
       const float corr = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       l *= corr;
