@@ -271,49 +271,10 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   const int64_t row_off = b * p.stride_b + h_own * p.stride_h + i_own * p.stride_n;
   const int limit = row_limit(p, seq, own);
   const int limit_wave = __builtin_amdgcn_readfirstlane(row_limit(p, seq, min(row0 + wave * 32 + 31, last_row)));
-  // q / 2^e in fp16, 2^e the power of two at the row's largest magnitude, in the order of a word's codes; qb: the groups' sums of that
-  f16x8 qf[D / 16], qb;
-  float c_row;  // logit scale times log2(e) times 2^e
-  {
-    uint4 raw[D / 16];
-    uint32_t top = 0u;
+  uint4 q_raw[D / 16];
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      raw[s] = *reinterpret_cast<const uint4*>(p.q + row_off + 16 * s + 8 * h);
-      const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
-    }
-    const u32x2 both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    const uint32_t e = min(max(max(both[0], both[1]) >> 23, 1u), 253u);
-    const float down = __uint_as_float((254u - e) << 23);
-    c_row = p.scale * __uint_as_float(e << 23);
-    float sum[D / G];
-#pragma unroll
-    for (int g = 0; g < D / G; ++g) sum[g] = 0.f;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = (i & 1 ? bf16_high(w[i / 2]) : bf16_low(w[i / 2])) * down;
-        const _Float16 y = (_Float16)x;
-        qf[s][i < 4 ? 2 * i : 2 * i - 7] = y;
-        sum[s * 16 / G] += (float)y;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {  // quarters 2 h and 2 h + 1
-      float t = 0.f;
-#pragma unroll
-      for (int g = 0; g < D / G; ++g) {
-        const float all = half_swap_sum(sum[g]);
-        if (2 * h + i == g) t = all;
-      }
-      const _Float16 hi = (_Float16)t, lo = (_Float16)(t - (float)hi);
-      qb[4 * i] = hi; qb[4 * i + 1] = lo; qb[4 * i + 2] = hi; qb[4 * i + 3] = (_Float16)0.f;
-    }
-  }
+  for (int s = 0; s < D / 16; ++s) q_raw[s] = *reinterpret_cast<const uint4*>(p.q + row_off + 16 * s + 8 * h);
+
   f32x16 o[D / 32];
 #pragma unroll
   for (int t = 0; t < D / 32; ++t) o[t] = f32x16{0};
@@ -417,6 +378,55 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
     for (int t = 0; t < 2 * (D / 32); ++t) at.va[t] = va[t] + (uint32_t)(x * TILE);
   };
 
+  if (t_begin < t_end) {  // K group -1 is requested
+    k_page = look_up(k_pos(-1));
+    raw.load_k(run_of(k_page), page, slot_of(k_pos(-1)), raw_at);
+    k_page = look_up(k_pos(0));
+    v_page = look_up(v_pos(0));
+  }
+
+  // q / 2^e in fp16, 2^e the power of two at the row's largest magnitude, in the order of a word's codes; qb: the groups' sums of that
+  f16x8 qf[D / 16], qb;
+  float c_row;  // logit scale times log2(e) times 2^e
+  {
+    uint32_t top = 0u;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const uint32_t w[4] = {q_raw[s].x, q_raw[s].y, q_raw[s].z, q_raw[s].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
+    }
+    const u32x2 both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    const uint32_t e = min(max(max(both[0], both[1]) >> 23, 1u), 253u);
+    const float down = __uint_as_float((254u - e) << 23);
+    c_row = p.scale * __uint_as_float(e << 23);
+    float sum[D / G];
+#pragma unroll
+    for (int g = 0; g < D / G; ++g) sum[g] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const uint32_t w[4] = {q_raw[s].x, q_raw[s].y, q_raw[s].z, q_raw[s].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = (i & 1 ? bf16_high(w[i / 2]) : bf16_low(w[i / 2])) * down;
+        const _Float16 y = (_Float16)x;
+        qf[s][i < 4 ? 2 * i : 2 * i - 7] = y;
+        sum[s * 16 / G] += (float)y;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {  // quarters 2 h and 2 h + 1
+      float t = 0.f;
+#pragma unroll
+      for (int g = 0; g < D / G; ++g) {
+        const float all = half_swap_sum(sum[g]);
+        if (2 * h + i == g) t = all;
+      }
+      const _Float16 hi = (_Float16)t, lo = (_Float16)(t - (float)hi);
+      qb[4 * i] = hi; qb[4 * i + 1] = lo; qb[4 * i + 2] = hi; qb[4 * i + 3] = (_Float16)0.f;
+    }
+  }
+
   // ---- a tile of which not every row sees every token; k, v: where its K and V are ----
   auto masked_tile = [&](int tile, int k, int v) {
     if (64 * tile >= limit_wave) return;  // none of the wave's rows sees any of it
@@ -484,10 +494,6 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
 
   if (t_begin < t_end) {
     // K groups -1 (for the first tile) and 0, V group 0; groups 1 requested
-    k_page = look_up(k_pos(-1));
-    raw.load_k(run_of(k_page), page, slot_of(k_pos(-1)), raw_at);
-    k_page = look_up(k_pos(0));
-    v_page = look_up(v_pos(0));
     cv.take_k(raw, quarter);
     request(0);
     store_k(-1);
