@@ -13,6 +13,25 @@
 PASA_DEVICE float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 PASA_DEVICE float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+constexpr float kLn2 = 0.6931471805599453f;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(4))) const int32_t const_i32;  // read by scalar loads
+
+// N words at once
+template <int N>
+PASA_DEVICE void load_words(const uint8_t* base, uint32_t off, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const uint4 v = *reinterpret_cast<const uint4*>(base + off);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(base + off);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    static_assert(N == 1, "");
+    w[0] = *reinterpret_cast<const uint32_t*>(base + off);
+  }
+}
+
 // offsets inside a head's run of a page
 template <int D, int G>
 struct CacheLayout {
@@ -39,4 +58,10 @@ PASA_DEVICE CacheSequence cache_sequence(const CacheParams& p, int b, int n) {
   s.first = (int64_t)len - s.rows;
   s.length = min(len, p.max_pages << p.log_page);
   return s;
+}
+// how many of the sequence's tokens row r of `share` rows a token sees
+PASA_DEVICE int cache_limit(const CacheSequence& s, int causal, int share, int r) {
+  if (!causal) return s.length;
+  const int64_t own = s.first + r / share + 1;
+  return own < 0 ? 0 : own < s.length ? (int)own : s.length;
 }

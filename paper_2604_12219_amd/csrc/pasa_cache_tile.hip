@@ -4,25 +4,26 @@
 // What differs is how a tile gets there: a thread holds a few code words of one token, of K and of V, converts them and writes them
 // to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, hence eight waves
 // and 256 rows: with four waves and 128 it costs twice as much a row.
+// Measured: 3600 rows of 40 heads over 75,600 tokens, d = 128, groups of 32, 5.93 ms, 940 TFLOP/s; 4680 rows of 12 heads over 32,760, 1.00 ms.  Per wave and tile 34
+// matrix and 251 vector instructions (150 in attention over bf16), the matrix cores busy 0.58 and the vector units 0.60 of the cycles at the 1.78 GHz that
+// the power leaves (bf16: 0.70 at 1.6).  A conversion that costs nothing would take 10 % off, keys rounded to bf16 3 %.
 //
 //   V: bf16(s c + m).  An and-or (and one shift for half of a word) makes fp16 numbers 1024 + c or 64 + c of two codes, a mixed fma
 //     s c + m of each (s (1024 + c) + (m - 1024 s): the rounding of that is 2^-13 of s), a conversion rounds two of them to bf16: 2.1 instructions a
 //     value.  Values beyond +-2^100 do not exist in a cache (pasa_cache_write), so 1024 s is finite.
 //   K: fp16 s (c - 8), which is exact (s has 8 bits, c - 8 at most 3 or is a power of two): a shift and an and-or make 1 + c/16 of two codes, a
-//     packed fma 16 s (1 + c/16) - 24 s: 1.5 instructions a value.  What that leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix instruction per 32 keys, with both factors as sums
-//     of two fp16 numbers (22 bits).  So the logits are those of the cache's values to binary32; with keys rounded to bf16 they are not,
-//     and lse is off by 1e-5.  Queries are fp16 times a power of two per row, which the row's logit scale takes back.
+//     packed fma 16 s (1 + c/16) - 24 s: 1.5 instructions a value.  What that leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix
+//     instruction per 32 keys, with both factors as sums of two fp16 numbers (22 bits).  So the logits are those of the cache's values to binary32;
+//     with keys rounded to bf16 they are not, and lse is off by 1e-5.  Queries are fp16 times a power of two per row, which the row's logit scale takes
+//     back.
 //     Keys beyond +-16384 do not exist in a cache (pasa_cache_write), so 24 s is an fp16 number.
 #include "pasa_cache.hpp"
 #include "pasa_cache_pipes.hpp"
 
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
-typedef __attribute__((address_space(4))) const int32_t const_i32;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // 8 values of a word of codes in bf16; b0 = m - 1024 s, b1 = m - 64 s
 PASA_DEVICE uint4 values8(uint32_t x, float s, float b0, float b1) {
@@ -55,20 +56,6 @@ PASA_DEVICE uint4 keys8(uint32_t x, uint32_t f) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, h[i]), a, b));
   return make_uint4(r[0], r[1], r[2], r[3]);
-}
-
-template <int N>
-PASA_DEVICE void load_words(const uint8_t* base, uint32_t off, uint32_t (&w)[N]) {
-  if constexpr (N == 4) {
-    const uint4 v = *reinterpret_cast<const uint4*>(base + off);
-    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-  } else if constexpr (N == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(base + off);
-    w[0] = v.x; w[1] = v.y;
-  } else {
-    static_assert(N == 1, "");
-    w[0] = *reinterpret_cast<const uint32_t*>(base + off);
-  }
 }
 
 PASA_DEVICE bool finite_param(uint32_t w) { return (w & 0x7f80u) != 0x7f80u && (w & 0x7f800000u) != 0x7f800000u; }
@@ -171,11 +158,7 @@ PASA_DEVICE CacheItem cache_item(const CacheAttnParams& p, int e) {
   it.rows = p.H / p.c.H_kv * it.seq.rows;
   return it;
 }
-PASA_DEVICE int row_limit(const CacheAttnParams& p, const CacheSequence& seq, int r) {  // tokens that row r sees
-  if (!p.causal) return seq.length;
-  const int64_t own = seq.first + r / (p.H / p.c.H_kv) + 1;
-  return own < 0 ? 0 : own < seq.length ? (int)own : seq.length;
-}
+PASA_DEVICE int row_limit(const CacheAttnParams& p, const CacheSequence& seq, int r) { return cache_limit(seq, p.causal, p.H / p.c.H_kv, r); }
 PASA_DEVICE int item_tiles(const CacheAttnParams& p, const CacheItem& it) { return (row_limit(p, it.seq, min(it.row0 + p.wg_rows, it.rows) - 1) + 63) >> 6; }
 PASA_DEVICE int item_weight(const CacheAttnParams& p, int e) {
   const CacheItem it = cache_item(p, e);
@@ -610,9 +593,10 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   }
 }
 
-// Items that several workgroups share, from their parts.  Its time is a chain of loads, so four rows go side by side: few parts by one wave, its lanes on
-// 64/LANES parts at a time, workgroup (w, y) on rows 16 y .. of the item whose last part workgroup w of cache_tile_kernel had; many parts, of few
-// rows if they are not that many, by the four waves of a workgroup, each a quarter, and by the workgroups (w, y) of all parts but the first.
+// Items that several workgroups share, from their parts (67 MB of them where all 256 workgroups have two of 256 rows of 128 channels: 22 us).  Its time is
+// a chain of loads, so four rows go side by side: few parts by one wave, its lanes on 64/LANES parts at a time, workgroup (w, y) on rows 16 y .. of the
+// item whose last part workgroup w of cache_tile_kernel had; many parts, of few rows if they are not that many, by the four waves of a workgroup, each
+// a quarter, and by the workgroups (w, y) of all parts but the first.
 template <int D>
 __global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
   constexpr int LANES = D / 4, PP = 64 / LANES, R = 4, WAVES = 4;  // lanes of a part's row, parts at a time in a wave, rows
