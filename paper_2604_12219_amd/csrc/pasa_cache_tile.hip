@@ -164,13 +164,15 @@ PASA_DEVICE int item_weight(const CacheAttnParams& p, int e) {
   const CacheItem it = cache_item(p, e);
   return it.row0 >= it.rows ? 0 : max(item_tiles(p, it), 1);
 }
-// the first item from e on that has rows (p.c.B * row_tiles if there is none)
-PASA_DEVICE int next_item(const CacheAttnParams& p, int e) {
+// the first item from e on that has rows (p.c.B * row_tiles if there is none); e is uniform, the lanes look at 64 sequences at once
+PASA_DEVICE int next_item(const CacheAttnParams& p, int e, int lane) {
   const int end = p.c.B * p.row_tiles;
-  while (e < end) {
-    const CacheItem it = cache_item(p, e);
-    if (it.row0 < it.rows) return e;
-    e = (it.b + 1) * p.row_tiles;
+  if (e >= end) return end;
+  const CacheItem it = cache_item(p, e);
+  if (it.row0 < it.rows) return e;
+  for (int b0 = it.b + 1; b0 < p.c.B; b0 += 64) {
+    const uint64_t there = __builtin_amdgcn_ballot_w64(b0 + lane < p.c.B && cache_sequence(p.c, min(b0 + lane, p.c.B - 1), p.n).rows > 0);
+    if (there != 0u) return (b0 + __builtin_ctzll(there)) * p.row_tiles;
   }
   return end;
 }
@@ -584,10 +586,10 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   }
   at += take_tiles;
   off = 0;
-  item = next_item(p, item + 1);
+  item = next_item(p, item + 1, lane);
   if (item == items) {
     ++hkv;
-    item = next_item(p, 0);
+    item = next_item(p, 0, lane);
   }
   item = __builtin_amdgcn_readfirstlane(item);
   }

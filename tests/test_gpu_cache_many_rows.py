@@ -55,6 +55,14 @@ def test_more_items_than_workgroups(P, causal):
     Wide(P, lens, [(53 * b) % 141 for b in range(80)], n=140, H=4, H_kv=4, d=64, group=64).fill().check(causal)
 
 
+def test_few_sequences_among_many_idle_ones(P):
+    lens, news = [0] * 400, [0] * 400
+    for b, length in ((3, 700), (4, 130), (70, 64), (255, 1290), (398, 5)):
+        lens[b], news[b] = length, min(length, 140)
+    lens[200] = 900  # tokens, no rows
+    Wide(P, lens, news, n=140, H=2, H_kv=2, d=64, group=32, page=1024).fill().check()
+
+
 @pytest.mark.parametrize("length, n, H, d, group", [(9000, 130, 1, 128, 32), (20011, 100, 2, 128, 64), (30000, 140, 1, 64, 32), (2900, 400, 1, 128, 128)])
 def test_one_sequence_in_many_parts(P, length, n, H, d, group):
     s = Wide(P, [length], [n], H=H, H_kv=H, d=d, group=group, page=256).fill()
