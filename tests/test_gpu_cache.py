@@ -168,6 +168,21 @@ def test_long_random_rows_round_as_in_64_bits(P):
     assert torch.equal(got, want)
 
 
+def test_ties_with_the_smallest_scales(P):
+    """scales of 2^-126 to 2^-120, whose products leave binary32's normal range; quotients in the middle between two codes wherever bf16 has them"""
+    s = Setup(P, [192], [192], H_kv=1, page=64)
+    scale = (torch.arange(0x80, 0x380, dtype=torch.int32) << 16).view(torch.float32).double()  # 768 groups, 192 rows of four
+    high = (15 * scale).float().bfloat16()
+    scale = (high.double() / 15).float().bfloat16().double()
+    x = torch.zeros(768, 32, dtype=torch.bfloat16)
+    x[:, 0] = high
+    x[:, 1:16] = ((torch.arange(15) + 0.5) * scale[:, None]).float().bfloat16()
+    x[:, 17:32] = ((torch.arange(15) + 0.5) * scale[:, None] * 0.99).float().bfloat16()
+    s.k[0, 0], s.v[0, 0] = x.view(192, 128), (x - high[:, None]).view(192, 128)
+    got, want = written(s, P)
+    assert torch.equal(got, want)
+
+
 # ---- reading back ------------------------------------------------------------------------------------
 @pytest.mark.parametrize("d, group", FORMATS)
 @pytest.mark.parametrize("token_major", [False, True])
