@@ -877,7 +877,7 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   if (ws_bytes < plan.total) return PASA_EWORKSPACE;
   p.q = static_cast<const uint16_t*>(q); p.o = static_cast<uint16_t*>(out); p.lse = lse;
   p.stride_b = shape->stride_b; p.stride_h = shape->stride_h; p.stride_n = shape->stride_n;
-  p.H = shape->H; p.n = shape->n; p.causal = causal != 0;
+  p.H = shape->H; p.share = shape->H / cache->H_kv; p.n = shape->n; p.causal = causal != 0;
   p.scale = effective_scale(shape) * 1.4426950408889634f;
   p.wg_rows = plan.wg_rows; p.splits = plan.splits;
   p.part_o = static_cast<float*>(ws);

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
   const int col = lane & 15, x = lane >> 4;
   const int split = blockIdx.x % p.splits, row0 = (int)(blockIdx.x / p.splits) * ROWS, hkv = blockIdx.y, b = blockIdx.z;
   const CacheSequence seq = cache_sequence(p.c, b, p.n);
-  const int share = p.H / p.c.H_kv, rows = share * seq.rows;
+  const int share = p.share, rows = share * seq.rows;
   if (row0 >= rows) return;
   const int last_row = min(row0 + ROWS, rows) - 1;
   auto limit_of = [&](int r) -> int { return cache_limit(seq, p.causal, share, r); };
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(256) cache_merge_kernel(CacheAttnParams p) {
 
 template <int D, int G>
 hipError_t launch_rows(const CacheAttnParams& p, hipStream_t stream) {
-  const int rows = p.H / p.c.H_kv * p.n;
+  const int rows = p.share * p.n;
   const dim3 grid((rows + p.wg_rows - 1) / p.wg_rows * p.splits, p.c.H_kv, p.c.B);
   if (p.wg_rows == 4) cache_rows_kernel<D, G, 1><<<grid, kWaves * 64, 0, stream>>>(p);
   else if (p.wg_rows == 8) cache_rows_kernel<D, G, 2><<<grid, kWaves * 64, 0, stream>>>(p);

@@ -32,7 +32,7 @@ struct CacheAttnParams {
   uint16_t* o;
   float* lse;  // nullable
   int64_t stride_b, stride_h, stride_n;
-  int32_t H, n, causal;
+  int32_t H, share, n, causal;  // share = H / H_kv
   float scale;  // of the logits, times log2(e)
   int32_t wg_rows;  // (row, head of a key/value head's share) pairs of a workgroup: 4, 8, 16 (pasa_cache_attn.hip) or 256 (pasa_cache_tile.hip)
   // 4, 8, 16: a sequence's tokens are divided among `splits` workgroups, at most kCacheMaxSplits, and with splits > 1

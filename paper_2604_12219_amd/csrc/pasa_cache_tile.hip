@@ -155,10 +155,10 @@ PASA_DEVICE CacheItem cache_item(const CacheAttnParams& p, int e) {
   it.b = e / p.row_tiles;
   it.row0 = (e % p.row_tiles) * p.wg_rows;
   it.seq = cache_sequence(p.c, it.b, p.n);
-  it.rows = p.H / p.c.H_kv * it.seq.rows;
+  it.rows = p.share * it.seq.rows;
   return it;
 }
-PASA_DEVICE int row_limit(const CacheAttnParams& p, const CacheSequence& seq, int r) { return cache_limit(seq, p.causal, p.H / p.c.H_kv, r); }
+PASA_DEVICE int row_limit(const CacheAttnParams& p, const CacheSequence& seq, int r) { return cache_limit(seq, p.causal, p.share, r); }
 PASA_DEVICE int item_tiles(const CacheAttnParams& p, const CacheItem& it) { return (row_limit(p, it.seq, min(it.row0 + p.wg_rows, it.rows) - 1) + 63) >> 6; }
 PASA_DEVICE int item_weight(const CacheAttnParams& p, int e) {
   const CacheItem it = cache_item(p, e);
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
 
   for (bool first_part = true; at < end; first_part = false) {
   const CacheItem it = cache_item(p, item);
-  const int b = it.b, row0 = it.row0, rows = it.rows, share = p.H / p.c.H_kv, last_row = min(row0 + ROWS, rows) - 1;
+  const int b = it.b, row0 = it.row0, rows = it.rows, share = p.share, last_row = min(row0 + ROWS, rows) - 1;
   const CacheSequence seq = it.seq;
   const int limit_all = __builtin_amdgcn_readfirstlane(row_limit(p, seq, row0)), limit_any = __builtin_amdgcn_readfirstlane(row_limit(p, seq, last_row));
   const int tiles = (limit_any + 63) >> 6, weight = max(tiles, 1);
@@ -613,7 +613,7 @@ __global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
   if (!shared && part != mg.parts - 1) return;
   const int r0 = (shared ? (part - 1) * (int)gridDim.y + (int)blockIdx.y : (int)blockIdx.y * WAVES + wave) * R;
   if (r0 > last) return;
-  const int share = p.H / p.c.H_kv, sub = lane / LANES, ch = lane % LANES * 4;
+  const int share = p.share, sub = lane / LANES, ch = lane % LANES * 4;
   // part 0 in slot first_slot, the others at the starts of the workgroups after that; rows behind the last one are the last one again, not written
   auto place = [&](int j, int k) -> int64_t {
     return (j == 0 ? mg.first_slot : (int64_t)2 * (mg.first_slot / 2 + j)) * p.wg_rows + min(r0 + k, last);
