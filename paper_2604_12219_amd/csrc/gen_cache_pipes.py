@@ -13,7 +13,7 @@ import gen_mfma_pipes as base
 from gen_mfma_pipes import FS_P0, FS_P1, FS_S0, FS_S1, FS_T, MFMA, NOP_AFTER, Cold, F, exp_stream, max_stream, off, pending, pour, vr
 
 MFMA_F16 = "v_mfma_f32_32x32x16_f16"
-BIAS_ROW = 32  # bytes of a key's offset operands
+BIAS_ROW = 32  # bytes of a key's offset operands: 16 for each half-wave, those of a tile's 64 keys for the first one, then for the other
 
 
 def growth(cold, flag, corr):
@@ -92,7 +92,7 @@ def run(D, mf, before, after, group=0, prologue=()):
         kind, a, b, tile = mf[k]["load"]
         at = (2 * group + tile) * 128 * D
         if kind == "b":  # offset operands of 32 keys
-            lines.append(f"ds_read_b128 {F(f)}, %[ab]{off((2 * (2 * group + tile) + b) * 32 * BIAS_ROW)}")
+            lines.append(f"ds_read_b128 {F(f)}, %[ab]{off((2 * group + tile) * 64 * BIAS_ROW + b * 32 * (BIAS_ROW // 2))}")
         elif kind == "k":
             lines.append(f"ds_read_b128 {F(f)}, %[ka{a}]{off(at + b * 64 * D)}")
         else:

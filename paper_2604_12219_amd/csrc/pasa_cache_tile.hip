@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   const uint32_t ring_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
   // the lane's addresses of the operand fetches in the first K tile, its offset operands and the first V tile
   uint32_t ka[D / 16], va[2 * (D / 32)];
-  const uint32_t ab = ring_base + (uint32_t)(4 * GROUP + ql * 32 + h * 16);
+  const uint32_t ab = ring_base + (uint32_t)(4 * GROUP + h * (BIAS / 2) + ql * 16);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) ka[s] = (ring_base + (uint32_t)lds_chunk_off<D>(ql, h)) ^ (uint32_t)(s << 5);
   {
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
     request(v + 1);
   };
   auto store_bias = [&](int v) {
-    *reinterpret_cast<uint2*>(ring + 4 * GROUP + (v & 1) * 2 * BIAS + k_token * 32 + quarter * 8) = cv.bias;
+    *reinterpret_cast<uint2*>(ring + 4 * GROUP + (2 * (v & 1) + (k_token >> 6)) * BIAS + (quarter >> 1) * (BIAS / 2) + (k_token & 63) * 16 + (quarter & 1) * 8) = cv.bias;
   };
   auto store_k = [&](int v) {
     store_bias(v);
