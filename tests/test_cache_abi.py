@@ -112,6 +112,28 @@ def test_arguments_are_checked_before_any_launch(P):
     attn(EWORKSPACE, nbytes=ctypes.c_size_t(0))
 
 
+def test_rows_that_cannot_be_numbered_are_refused(P):
+    """2^31 (row, head) pairs of one key/value head"""
+    L = P.load_library()
+    c, s = ctypes.byref(_cache(P, H_kv=1).c()), ctypes.byref(_shape(P, H=65535, n=1 << 15, stride_h=128, stride_n=128).c())
+    assert L.pasa_cache_attn_workspace_bytes(s, c, 0) == 0
+    assert L.pasa_cache_attn(A, s, c, A, BIG, A, A, None, 0, 0, B_, None, A, BIG, None) == EUNSUPPORTED
+
+
+@pytest.mark.parametrize("B, H, H_kv, n", [(1, 1, 1, 1), (65535, 1, 1, 1), (1, 65535, 65535, 9), (1, 65535, 1, 1), (1, 8, 8, 1 << 23), (255, 257, 1, 16), (4095, 16, 2, 100)])
+@pytest.mark.parametrize("n_max", [0, 1, 1000, 2 ** 31 - 1])
+def test_workspaces_at_the_ends_of_the_ranges(P, B, H, H_kv, n, n_max):
+    """at most 64 parts of every row, or two parts of 256 rows of 256 workgroups"""
+    for d, group in ((64, 32), (128, 32), (128, 128)):
+        c = _cache(P, H_kv=H_kv, d=d, group=group, page=1024, max_pages=1 << 20)
+        s = _shape(P, B=B, H=H, n=n, d=d, stride_n=d)
+        got = P.cache_attn_workspace_bytes(s, c, n_max)
+        most = max(64 * B * H * n, 2 * 256 * 256) * (d + 2) * 4 + 16384
+        assert 0 < got <= most
+        if B * H * n > 1 << 22:  # far more rows than there is anything to divide for
+            assert got < 1 << 28
+
+
 def test_the_binding_refuses_what_the_library_cannot_see(P):
     cache, shape = _cache(P), _shape(P, n=5)
     rows = torch.zeros(1, 2, 5, 128, dtype=torch.bfloat16)
