@@ -31,6 +31,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 PASA_DEVICE f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
     uint16_t w[kWaves][NG][ROWS][64];
   };
   struct Result {
-    float o[kWaves][ROWS][D];
+    float o[kWaves][ROWS][D + 4];  // (4 more: the four rows that a wave writes at once fall into different banks)
     float m[kWaves][ROWS], l[kWaves][ROWS];
   };
   __shared__ __attribute__((aligned(16))) union { Work work; Result res; } sh;
@@ -351,28 +352,34 @@ __global__ void __launch_bounds__(kWaves * 64, 2) cache_rows_kernel(CacheAttnPar
     if (col == 0) { sh.res.m[wave][r] = m[i]; sh.res.l[wave][r] = l[i]; }
   }
   __syncthreads();
-  for (int e = tid; e < ROWS * D; e += kWaves * 64) {
-    const int r = e / D, ch = e % D;
+  constexpr int TPR = D / 4;  // threads of a row, four channels each
+  for (int r = tid / TPR; r < ROWS; r += kWaves * 64 / TPR) {
+    const int ch = tid % TPR * 4;
     if (row0 + r > last_row) break;
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.res.m[w][r]);
     const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, val = 0.f;
+    float sum = 0.f;
+    f32x4 val = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float f = __builtin_amdgcn_exp2f(sh.res.m[w][r] - ref);
+      const f32x4 part = *reinterpret_cast<const f32x4*>(&sh.res.o[w][r][ch]);
       sum = fmaf(f, sh.res.l[w][r], sum);
-      val = fmaf(f, sh.res.o[w][r][ch], val);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) val[i] = fmaf(f, part[i], val[i]);
     }
     const RowPlace at = row_place(p, b, hkv, share, row0 + r);
     if (p.splits == 1) {  // a row that sees nothing is zero, its normaliser empty
-      const __bf16 y = (__bf16)(sum == 0.f ? 0.f : val / sum);
-      p.o[at.out + ch] = __builtin_bit_cast(uint16_t, y);
+      bf16x4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = (__bf16)(sum == 0.f ? 0.f : val[i] / sum);
+      *reinterpret_cast<bf16x4*>(p.o + at.out + ch) = y;
       if (p.lse && ch == 0) p.lse[at.lse] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     } else {
       const int64_t part = at.lse * p.splits + split;
-      p.part_o[part * D + ch] = val;
+      *reinterpret_cast<f32x4*>(p.part_o + part * D + ch) = val;
       if (ch == 0) { p.part_ml[2 * part] = top; p.part_ml[2 * part + 1] = sum; }
     }
   }
