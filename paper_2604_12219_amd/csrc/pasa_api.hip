@@ -794,13 +794,13 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
   // 4, 8 or 16 rows a workgroup (cache_rows_kernel) take time with the runs of 16 rows and the tiles of 64 tokens: 0.0024 us each with groups of 32 of
-  // 128 channels, 0.0021 with groups of 64, 0.0013 with one of 128, 0.0012 with 64 channels.  256 rows (cache_tile_kernel) take time with the tiles, 0.0093
-  // us, 0.0058 with 64 channels, and some 28 us more before and after them.  us, 16 rows / 256:
-  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 17.0 / 28.0, 500 rows 18.7 / 34.5; 1 head, 200,000 tokens, 33 rows 55 / 114; 40,000, 128 rows
-  //     31 / 54; 8 heads of 20,000, 100 rows 55 / 68; 64 heads of 4000, 33 rows 50 / 76, 64 55 / 78, 128 84 / 84, 192 133 / 94; 40 heads of 75,600, 40
-  //     rows 350 / 447, 64 472 / 453
-  //   groups of 64: 64 heads of 4000, 33 rows 39 / 74; of 128: 64 rows 40 / 75, 128 57 / 81
-  //   d = 64: 64 heads of 4000, 33 rows 26 / 47, 64 34 / 49, 128 47 / 53, 200 79 / 57; 40 heads of 75,600, 64 rows 220 / 281
+  // 128 channels, 0.002 with groups of 64, 0.0013 with one of 128, 0.0012 with 64 channels.  256 rows (cache_tile_kernel) take time with the tiles, 0.009 us,
+  // 0.0055 with 64 channels, and some 25 us more before and after them.  us, 16 rows / 256:
+  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 17 / 27, 500 rows 18 / 32; 1 head, 200,000 tokens, 33 rows 54 / 107; 40,000, 128 rows 29 / 51; 8
+  //     heads of 20,000, 100 rows 52 / 65; 64 heads of 4000, 33 rows 47 / 70, 64 52 / 71, 128 81 / 78, 192 127 / 84; 40 heads of 75,600, 40 rows 345 / 429,
+  //     64 467 / 437
+  //   groups of 64: 64 heads of 4000, 33 rows 37 / 71; of 128: 64 rows 38 / 68, 128 54 / 75
+  //   d = 64: 64 heads of 4000, 33 rows 25 / 44, 64 32 / 46, 128 45 / 49, 200 77 / 52; 40 heads of 75,600, 64 rows 217 / 270
   const double head_tiles = (double)s->B * c->H_kv * ((tokens + 63) / 64), weight = c->group == 128 ? 2 : s->d == 128 && c->group == 32 ? 4 : 3;
   a.row_tiles = (int)((rows + 255) / 256);
   const bool few = weight * head_tiles * ((rows + 15) / 16) <= 49152 + 14 * head_tiles * a.row_tiles;
@@ -824,8 +824,8 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
     }
     if (a.splits > 1) parts = (size_t)s->B * s->H * s->n * a.splits;
   } else {
-    // one for every compute unit, and if there are fewer than four heads' runs of rows, 64 for each: one head of 40,000 tokens, 40 rows 55 us with 64,
-    // 61 with 32, 66 with 128
+    // one for every compute unit, and if there are fewer than four heads' runs of rows, 64 for each: one head of 40,000 tokens, 128 rows 59 us with 64,
+    // 64 with 32, 69 with 128
     a.pieces = (int)std::min<int64_t>(256, 64 * (int64_t)s->B * c->H_kv * a.row_tiles);
     parts = (size_t)2 * a.pieces * a.wg_rows;
   }

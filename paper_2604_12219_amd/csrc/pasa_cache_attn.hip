@@ -20,8 +20,8 @@
 //   Values: A = weights, B = V codes (columns: channels).  The transposing 4-bit LDS read hands a lane 16 tokens of one channel.
 //   A lane's weights of the tokens 16 t + (lane & 15), t = 0..3, are neighbours in the contraction, so they leave as one 8-byte LDS write.
 //   Measured: one token of 75,600, 40 heads of 128 channels, 484 MB in 92 us, 5.3 TB/s; 32 sequences of 800 to 8000 tokens, 8 heads with 4 query heads each,
-//   184 MB in 39 us, 4.7 TB/s.  With 16 rows vector instructions bound it, some 540 a wave and tile with one group a head and 900 with four: 64 heads of
-//   4000 tokens, 33 rows each (three runs of 16), 45 us.
+//   184 MB in 38 us, 4.8 TB/s.  With 16 rows vector instructions bound it, some 540 a wave and tile with one group a head and 900 with four: 64 heads of
+//   4000 tokens, 33 rows each (three runs of 16), 47 us with the launch.
 // Longer sequences are divided among workgroups, each leaving (m, l, o), and cache_merge_kernel puts these together.
 #include "pasa_cache.hpp"
 
