@@ -185,7 +185,9 @@ def gen():
 
         def emit(comment, head, pre, lines, outs, ins, clob):
             text = "\n".join(f'      "{l}\\n\\t"' for l in lines)
-            regs = ", ".join([f'"v{r}"' for r in clob] + ['"memory"', '"scc"', '"vcc"'])
+            # No "memory": the compiler's waits for loads in flight, those of spilled values among them, leave out the pinned registers of statements that
+            # have it, and such a load can arrive on top of a result.  The ring's order is that of the barriers, which do say so.
+            regs = ", ".join([f'"v{r}"' for r in clob] + ['"scc"', '"vcc"'])
             out.append(f"{comment}PASA_DEVICE void {head} {{\n{pre}  asm volatile(\n{text}\n      : {', '.join(outs)}\n      : {', '.join(ins)}\n"
                        f"      : {regs});\n}}\n\n")
 
