@@ -378,7 +378,9 @@ PASA_API int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cach
  * O = softmax(Q K^T * scale) V over the cached tokens t < len[b]; with causal != 0 a row sees the tokens up to and including its own
  * only.  shape->H is a multiple of H_kv: head h attends over key/value head h / (H / H_kv).  A row that sees no token is zero, its lse -inf.
  * A row that sees a token of which a group reads back as NaN is NaN, lse included, if it is a group of K, and NaN in the channels of that
- * group, perhaps in others, if it is one of V.  Logits are held in binary32: beyond +-2^30 their spacing makes the weights overflow.
+ * group, perhaps in others, if it is one of V.  Logits are held in binary32: beyond +-2^30 their spacing makes the weights overflow.  They are
+ * good to what binary32 leaves of sum |q| |k|, whatever the magnitudes of q and of the groups of K are, and where calls of many rows are concerned to 2^-26
+ * of the largest product |q| |k| that the row makes with any group of the sequence's keys.
  *   q, out  bf16 [B, H, n, d] (shape strides);  lse fp32 [B*H, n] or NULL
  *   n_max   host: what len is expected not to exceed, 0 for max_pages * page.  The work is divided for this length; longer
  *           sequences are computed as well, only more slowly.

@@ -223,7 +223,7 @@ def gen():
         arr = f"const uint32_t (&%s)[{words}]"
         emit("// Two steps: P V of the two tiles of V group `group`, logits of the two of K group `group`, which are one tile further on; addresses are those of\n"
              f"// group 0.  Meanwhile {words} code words of K and of V are converted and written to the other groups: kc, vc the words, kf 16 s and\n"
-             "// -24 s of a K word's group as two fp16 numbers, vs, vm0, vm1 s, m - 1024 s and m - 64 s of the V words, kst, vst the lane's addresses\n",
+             "// -24 s of a K word's group, times a power of two, as two fp16 numbers, vs, vm0, vm1 s, m - 1024 s and m - 64 s of the V words, kst, vst the lane's addresses\n",
              f"pipe_steps(int group, {k_args}, {v_args}, {q_args}, {state}, float c,\n"
              f"                            {arr % 'kc'}, {arr % 'kf'}, {arr % 'vc'}, float vs, float vm0, float vm1, uint32_t kst, uint32_t vst)",
              "  uint64_t flag1;\n", base.both_parities("ps", lambda group: pipe_steps(D, words, group, 2)), step_outs, kin + vin + cin + group_in + conv,

@@ -786,8 +786,8 @@ bool cache_rows_fit(const pasa_shape_t* s, const pasa_cache_t* c) {
 
 // How the rows and tokens of a call are divided among workgroups, and the workspace that takes
 struct CacheAttnPlan {
-  int wg_rows, splits, pieces, row_tiles;
-  size_t part_ml, merge, total;
+  int wg_rows, splits, pieces, row_tiles, key_parts;
+  size_t part_ml, merge, key_range, total;
 };
 CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int32_t n_max) {
   CacheAttnPlan a{};
@@ -828,10 +828,23 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
     // 64 with 32, 69 with 128
     a.pieces = (int)std::min<int64_t>(256, 64 * (int64_t)s->B * c->H_kv * a.row_tiles);
     parts = (size_t)2 * a.pieces * a.wg_rows;
+    // K's magnitudes: runs of a thousand tokens, one pass of a workgroup's threads, unless that are more than the chip takes at once
+    a.key_parts = (int)std::max<int64_t>(1, std::min<int64_t>({kCacheMaxKeyParts, 1024 / ((int64_t)s->B * c->H_kv), (tokens + 1023) / 1024}));
   }
   a.part_ml = align_up(parts * s->d * 4);
   a.merge = align_up(a.part_ml + parts * 2 * 4);
-  a.total = align_up(a.merge + a.pieces * sizeof(CacheMerge) + 1);  // never zero: that means "invalid"
+  size_t end = a.merge + a.pieces * sizeof(CacheMerge) + 1;  // never zero: that means "invalid"
+  if (a.wg_rows == 256) {
+    // They have the place of the last workgroup's second part, which there never is: what that workgroup starts it also finishes.  More than that holds
+    // go behind everything else.
+    const size_t slot = (size_t)a.wg_rows * s->d * 4, range = (size_t)s->B * c->H_kv * a.key_parts * 4;
+    a.key_range = (2 * a.pieces - 1) * slot;
+    if (range > slot) {
+      a.key_range = align_up(end);
+      end = a.key_range + range;
+    }
+  }
+  a.total = align_up(end);
   return a;
 }
 }  // namespace
@@ -884,6 +897,8 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.part_ml);
   p.pieces = plan.pieces; p.row_tiles = plan.row_tiles;
   p.merge = reinterpret_cast<CacheMerge*>(static_cast<char*>(ws) + plan.merge);
+  p.key_range = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + plan.key_range);
+  p.key_parts = plan.key_parts;
   return pasa_launch_cache_attn(p, static_cast<hipStream_t>(stream)) == hipSuccess ? PASA_OK : PASA_EHIP;
 }
 

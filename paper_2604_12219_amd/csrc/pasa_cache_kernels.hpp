@@ -42,7 +42,10 @@ struct CacheAttnParams {
   // 256: all the work is divided among `pieces` workgroups; part_o, part_ml are [2 pieces][wg_rows][d], [..][2]
   int32_t pieces, row_tiles;  // row_tiles = runs of wg_rows rows that a sequence can have
   CacheMerge* merge;          // [pieces]
+  uint32_t* key_range;        // [B][H_kv][key_parts]: largest magnitudes of K's groups (pasa_cache_tile.hip), each of a run of a sequence's tokens
+  int32_t key_parts;          // at most kCacheMaxKeyParts
 };
+constexpr int kCacheMaxKeyParts = 64;  // a wave of cache_tile_kernel holds one per lane
 constexpr int kCacheMinPiece = 2;  // tiles of a piece, at least
 constexpr int kCacheMaxSplits = 64;  // a wave of the merging kernel holds one per lane
 hipError_t pasa_launch_cache_tiles(const CacheAttnParams& p, hipStream_t stream);  // wg_rows 256

@@ -11,12 +11,15 @@
 //   V: bf16(s c + m).  An and-or (and one shift for half of a word) makes fp16 numbers 1024 + c or 64 + c of two codes, a mixed fma
 //     s c + m of each (s (1024 + c) + (m - 1024 s): the rounding of that is 2^-13 of s), a conversion rounds two of them to bf16: 2.1 instructions a
 //     value.  Values beyond +-2^100 do not exist in a cache (pasa_cache_write), so 1024 s is finite.
-//   K: fp16 s (c - 8), which is exact (s has 8 bits, c - 8 at most 3 or is a power of two): a shift and an and-or make 1 + c/16 of two codes, a
-//     packed fma 16 s (1 + c/16) - 24 s: 1.5 instructions a value.  What that leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix
-//     instruction per 32 keys, with both factors as sums of two fp16 numbers (22 bits).  So the logits are those of the cache's values to binary32;
-//     with keys rounded to bf16 they are not, and lse is off by 1e-5.  Queries are fp16 times a power of two per row, which the row's logit scale takes
-//     back.
-//     Keys beyond +-16384 do not exist in a cache (pasa_cache_write), so 24 s is an fp16 number.
+//   K: fp16 2^f s (c - 8): a shift and an and-or make 1 + c/16 of two codes, a packed fma 16 s (1 + c/16) - 24 s: 1.5 instructions a value.  What that
+//     leaves out, sum_g (m_g + 8 s_g) sum_{i in g} q_i, is one more matrix instruction per 32 keys, with both factors as sums of two fp16 numbers
+//     (22 bits).  With keys rounded to bf16 instead lse would be off by 1e-5.
+//   Powers of two.  s has 8 bits and c - 8 at most 3 or is a power of two, so s (c - 8) is exact where fp16 has the exponents for it: s from 2^-17 to
+//     2^11.  A cache holds scales down to 2^-126.  So the groups of a key/value head are shifted to the top of fp16's range, each by the power 2^f that
+//     its largest operand over the sequence's tokens allows (cache_key_range_kernel; 2^13 to 2^14 then), and the queries by 2^-f; a row's queries
+//     then by one more power that puts the largest of them between 2^7 and 2^8 (the sum of 128 is an fp16 number), which the row's logit scale takes
+//     back.  So K is exact down to 2^-30 of a group's largest scale and q down to 2^-24 of the row's largest; what is smaller is rounded to 2^-25, that is
+//     2^-38 and 2^-32 of the largest.
 #include "pasa_cache.hpp"
 #include "pasa_cache_pipes.hpp"
 
@@ -101,19 +104,24 @@ struct Quarter {
     v_par = w[0];
   }
 };
+// 2^f of K's groups: 16 2^f and -24 2^f of each, 2^f of the lane's own quarter's
+template <int NG>
+struct KeyFactors {
+  float f16[NG], f24[NG], own;
+};
 // the same, taken for conversion
 template <int D, int G>
 struct Taken {
   typedef CacheLayout<D, G> L;
   static constexpr int N = D / 32;
-  uint32_t kc[N], kf[N], vc[N], v_par;  // kf: 16 s and -24 s of a K word's group in fp16
+  uint32_t kc[N], kf[N], vc[N], v_par;  // kf: 2^f times 16 s and -24 s of a K word's group in fp16
   float vs, vm0, vm1;                   // s, m - 1024 s, m - 64 s of the V words' group
-  uint2 bias;  // the token's offset operands of group q: (hi, hi, lo, 0) of m + 8 s, to be multiplied with (hi, lo, hi, 0) of the group's sum of q
-  PASA_DEVICE void take_k(const Quarter<D, G>& x, int q) {
+  uint2 bias;  // the token's offset operands of group q: (hi, hi, lo, 0) of 2^f (m + 8 s), to be multiplied with (hi, lo, hi, 0) of the group's sum of q
+  PASA_DEVICE void take_k(const Quarter<D, G>& x, int q, const KeyFactors<D / G>& up) {
     uint32_t own = x.k_par[0];
 #pragma unroll
     for (int g = 1; g < L::NG; ++g) own = q == g ? x.k_par[g] : own;
-    const float mid = fmaf(8.f, bf16_low(own), bf16_high(own));
+    const float mid = fmaf(8.f, bf16_low(own), bf16_high(own)) * up.own;
     const _Float16 hi = (_Float16)mid, lo = (_Float16)(mid - (float)hi);
     const f16x2 x0 = {hi, hi}, x1 = {lo, (_Float16)0.f};
     bias = make_uint2(__builtin_bit_cast(uint32_t, x0), __builtin_bit_cast(uint32_t, x1));
@@ -121,7 +129,7 @@ struct Taken {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float s = bf16_low(x.k_par[j * 32 / G]);
-      const f16x2 f = {(_Float16)(16.f * s), (_Float16)(-24.f * s)};
+      const f16x2 f = {(_Float16)(up.f16[j * 32 / G] * s), (_Float16)(up.f24[j * 32 / G] * s)};
       kf[j] = __builtin_bit_cast(uint32_t, f);
       kc[j] = x.k_code[j];
     }
@@ -139,13 +147,77 @@ struct Taken {
   }
 };
 
+// The largest magnitude of an operand that K makes, max(8 |s|, |m + 8 s|), of every group of a head over the sequence's tokens, as its biased exponent (0:
+// all are zero), byte g of a word for group g; parameters that are not finite do not count.  Workgroup (j, head, sequence) takes the j-th of key_parts
+// runs of tokens.  Bound by a chain of loads (length, page, parameters): 12 heads of 32,760 tokens 5 us, 40 heads of 75,600, 48 MB of parameters, 11 us.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+PASA_DEVICE uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+constexpr int kRangeThreads = 256;
+template <int D, int G>
+__global__ void __launch_bounds__(kRangeThreads) cache_key_range_kernel(CacheAttnParams p) {
+  typedef CacheLayout<D, G> L;
+  constexpr int NG = D / G, U = 4, WAVES = kRangeThreads / 64;
+  __shared__ uint32_t s_even[WAVES], s_odd[WAVES];
+  const int j = blockIdx.x, hkv = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  const CacheSequence seq = cache_sequence(p.c, b, p.n);
+  const int per = (seq.length + p.key_parts - 1) / p.key_parts, first = j * per, last = seq.rows > 0 ? min(first + per, seq.length) : 0;
+  const uint32_t page = 1u << p.c.log_page;
+  const int32_t* const table = p.c.pages + (int64_t)b * p.c.max_pages;
+  float top[NG];
+#pragma unroll
+  for (int g = 0; g < NG; ++g) top[g] = 0.f;
+  for (int at = first; at < last; at += U * kRangeThreads) {  // (the threads behind the last token look at that one again)
+    int pos[U], pg[U];
+    uint32_t w[U][NG];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      pos[u] = min(at + u * kRangeThreads + tid, last - 1);
+      pg[u] = table[pos[u] >> p.c.log_page];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool ok = pg[u] >= 0 && pg[u] < p.c.n_pages;
+      const uint8_t* const run = p.c.pool + ((int64_t)(ok ? pg[u] : 0) * p.c.H_kv + hkv) * p.c.head_bytes;
+      load_words<NG>(run, L::k_params(page) + ((uint32_t)pos[u] & (page - 1u)) * L::PARAM, w[u]);
+      if (!ok)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) w[u][g] = 0u;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const float s = bf16_low(w[u][g]), m = bf16_high(w[u][g]), size = fmaxf(8.f * fabsf(s), fabsf(fmaf(8.f, s, m)));
+        if (finite_param(w[u][g])) top[g] = fmaxf(top[g], size);
+      }
+  }
+  uint32_t pair[2] = {0u, 0u};  // groups 0 and 2, 1 and 3
+#pragma unroll
+  for (int g = 0; g < NG; ++g) pair[g & 1] |= (top[g] == 0.f ? 0u : max(__float_as_uint(top[g]) >> 23, 1u)) << (8 * (g & 2));
+  for (int d = 32; d >= 1; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) pair[i] = max_u16x2(pair[i], (uint32_t)__shfl_xor((int)pair[i], d));
+  if ((tid & 63) == 0) { s_even[tid >> 6] = pair[0]; s_odd[tid >> 6] = pair[1]; }
+  __syncthreads();
+  if (tid != 0) return;
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) {
+    pair[0] = max_u16x2(pair[0], s_even[w]);
+    pair[1] = max_u16x2(pair[1], s_odd[w]);
+  }
+  p.key_range[((int64_t)b * p.c.H_kv + hkv) * p.key_parts + j] = pair[0] | (pair[1] << 8);
+}
+
 // ---- who does what ----
 // An item is a (sequence, run of ROWS rows), numbered e = b * row_tiles + run, of one key/value head; its weight is the number of tiles that its rows
 // see (at least one where there are rows: somebody has to write them).  All items of all heads in a row, head by head, are a line of
 // tiles that the workgroups divide evenly, each a piece of `piece` of them: so an item can be shared by several workgroups, and the last ones have no
 // less to do than the first, whatever the lengths are (they are known on the device only).  Against one workgroup an item: 40 heads of 15 items,
 // 600 workgroups on 256 compute units, 14,400 rows and 75,600 tokens, 7640 -> 6300 us.
-// A workgroup's piece holds at most two parts of items: one at its start (slot 2 w of the partial results) and one at its end (slot 2 w + 1).
+// A workgroup's piece holds at most two parts of items: one at its start (slot 2 w of the partial results) and one at its end (slot 2 w + 1).  The last
+// workgroup's end is the end of an item: its second slot holds K's magnitudes (cache_attn_plan).
 struct CacheItem {
   int b, row0, rows;  // rows: of the sequence, times the share of heads
   CacheSequence seq;
@@ -259,6 +331,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   uint4 q_raw[D / 16];
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) q_raw[s] = *reinterpret_cast<const uint4*>(p.q + row_off + 16 * s + 8 * h);
+  uint32_t range = lane < p.key_parts ? p.key_range[((int64_t)b * p.c.H_kv + hkv) * p.key_parts + lane] : 0u;
 
   f32x16 o[D / 32];
 #pragma unroll
@@ -312,6 +385,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
   auto slot_of = [&](int pos) -> uint32_t { return (uint32_t)pos & (page - 1u); };
   int k_page, v_page;  // of the groups to be requested next
   Taken<D, G> cv;
+  KeyFactors<D / G> up;
   auto request = [&](int v) {  // groups v, whose pages have been looked up
     raw.load_k(run_of(k_page), page, slot_of(k_pos(v)), raw_at);
     raw.load_v(run_of(v_page), page, slot_of(v_pos(v)), raw_at);
@@ -319,7 +393,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
     v_page = look_up(v_pos(v + 1));
   };
   auto take = [&](int v) {  // the groups v, which have been requested; the ones after them are
-    cv.take_k(raw, quarter);
+    cv.take_k(raw, quarter, up);
     cv.take_v(raw);
     request(v + 1);
   };
@@ -370,21 +444,49 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
     v_page = look_up(v_pos(0));
   }
 
-  // q / 2^e in fp16, 2^e the power of two at the row's largest magnitude, in the order of a word's codes; qb: the groups' sums of that
-  f16x8 qf[D / 16], qb;
-  float c_row;  // logit scale times log2(e) times 2^e
+  // the powers of two of K's groups: the largest operand between 2^13 and 2^14, so that 24 s is an fp16 number (2^120 at most: 24 s 2^f in binary32)
+  constexpr int NG = D / G;
+  constexpr int kNoKeys = 1 << 12;  // of a group whose keys are zero: q does not matter and becomes zero
+  int f[NG];
   {
-    uint32_t top = 0u;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      const uint32_t w[4] = {q_raw[s].x, q_raw[s].y, q_raw[s].z, q_raw[s].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
+    uint32_t even = range & 0x00ff00ffu, odd = (range >> 8) & 0x00ff00ffu;
+    for (int d = 32; d >= 1; d >>= 1) {
+      even = max_u16x2(even, (uint32_t)__shfl_xor((int)even, d));
+      odd = max_u16x2(odd, (uint32_t)__shfl_xor((int)odd, d));
     }
-    const u32x2 both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    const uint32_t e = min(max(max(both[0], both[1]) >> 23, 1u), 253u);
-    const float down = __uint_as_float((254u - e) << 23);
-    c_row = p.scale * __uint_as_float(e << 23);
+    even = __builtin_amdgcn_readfirstlane(even);
+    odd = __builtin_amdgcn_readfirstlane(odd);
+    up.own = 0.f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int e = (int)(((g & 1 ? odd : even) >> (8 * (g & 2))) & 0xffu), own_f = min(140 - e, 120);
+      f[g] = e == 0 ? kNoKeys : own_f;
+      const uint32_t pow16 = (uint32_t)(own_f + 131) << 23;  // (put together from bits, so that they are scalars)
+      up.f16[g] = __uint_as_float(pow16);
+      up.f24[g] = __uint_as_float(pow16 | 0x80400000u);
+      if (quarter == g) up.own = __uint_as_float((uint32_t)(own_f + 127) << 23);
+    }
+  }
+  // 2^(7 - e - f) q in fp16, 2^e the power of two at the largest 2^-f |q| of the row, in the order of a word's codes; qb: the groups' sums of that
+  f16x8 qf[D / 16], qb;
+  float c_row;  // logit scale times log2(e) times 2^(e - 7)
+  {
+    int e = -kNoKeys;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      uint32_t top = 0u;
+#pragma unroll
+      for (int s = g * (G / 16); s < (g + 1) * (G / 16); ++s) {
+        const uint32_t w[4] = {q_raw[s].x, q_raw[s].y, q_raw[s].z, q_raw[s].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
+      }
+      const u32x2 both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+      top = max(both[0], both[1]);
+      if (top != 0u && f[g] != kNoKeys) e = max(e, (int)max(top >> 23, 1u) - 127 - f[g]);
+    }
+    if (e == -kNoKeys) e = 0;
+    c_row = __builtin_ldexpf(p.scale, e - 7);
     float sum[D / G];
 #pragma unroll
     for (int g = 0; g < D / G; ++g) sum[g] = 0.f;
@@ -393,8 +495,8 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
       const uint32_t w[4] = {q_raw[s].x, q_raw[s].y, q_raw[s].z, q_raw[s].w};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = (i & 1 ? bf16_high(w[i / 2]) : bf16_low(w[i / 2])) * down;
-        const _Float16 y = (_Float16)x;
+        const float x = i & 1 ? bf16_high(w[i / 2]) : bf16_low(w[i / 2]);
+        const _Float16 y = (_Float16)__builtin_ldexpf(x, 7 - e - f[s * 16 / G]);
         qf[s][i < 4 ? 2 * i : 2 * i - 7] = y;
         sum[s * 16 / G] += (float)y;
       }
@@ -479,7 +581,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
 
   if (t_begin < t_end) {
     // K groups -1 (for the first tile) and 0, V group 0; groups 1 requested
-    cv.take_k(raw, quarter);
+    cv.take_k(raw, quarter, up);
     request(0);
     store_k(-1);
     take(0);
@@ -681,6 +783,7 @@ __global__ void __launch_bounds__(256) cache_merge_items(CacheAttnParams p) {
 
 template <int D, int G>
 hipError_t launch(const CacheAttnParams& p, hipStream_t stream) {
+  cache_key_range_kernel<D, G><<<dim3(p.key_parts, p.c.H_kv, p.c.B), kRangeThreads, 0, stream>>>(p);
   cache_tile_kernel<D, G><<<p.pieces, kTileWaves * 64, 0, stream>>>(p);
   cache_merge_items<D><<<dim3(p.pieces, p.wg_rows / 16), 256, 0, stream>>>(p);
   return hipGetLastError();
