@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kTileWaves * 64, 2) cache_tile_kernel(CacheAtt
       if (top != 0u && f[g] != kNoKeys) e = max(e, (int)max(top >> 23, 1u) - 127 - f[g]);
     }
     if (e == -kNoKeys) e = 0;
-    c_row = __builtin_ldexpf(p.scale, e - 7);
+    c_row = fmaxf(__builtin_ldexpf(p.scale, e - 7), 0x1p-126f);  // (never zero: -inf, the logit of a key that is not seen, has to stay that)
     float sum[D / G];
 #pragma unroll
     for (int g = 0; g < D / G; ++g) sum[g] = 0.f;

@@ -174,6 +174,29 @@ def test_groups_of_zeros_and_of_nan(P, n):
     check(s)
 
 
+@pytest.mark.parametrize("n", ROWS)
+@pytest.mark.parametrize("length", [1, 37, 64, 150])
+@pytest.mark.parametrize("scale", [1e-3, 1e-9, 1e-30, 1e-45])
+def test_small_scales(P, n, length, scale):
+    """rows of zeros and of small numbers in tiles with tokens that are not seen, rows that see nothing"""
+    for causal in (False, True):
+        s = setup_written(P, [length, 0], n, H=1, H_kv=1, page=64) if not causal else setup_written(P, [length, 1], n, H=1, H_kv=1, page=64)
+        s.q[0, 0, 0] = 0.0
+        if n > 2:
+            s.q[0, 0, 2] *= 2.0 ** -100
+        check(s, causal, scale)
+
+
+def test_rows_ahead_of_the_first_token_with_a_small_scale(P):
+    s = Wide(P, [5, 90], [140, 140], n=140, H=1, H_kv=1, page=64).fill()
+    s.q[:, :, ::2] = 0.0
+    out, lse = s.attend(causal=True, scale=1e-9)
+    assert torch.isinf(lse[0, 0, :135]).all() and not out[0, 0, :135].any()
+    assert torch.isinf(lse[1, 0, :50]).all() and not out[1, 0, :50].any()
+    seen = torch.cat([lse[0, 0, 135:], lse[1, 0, 50:]])
+    assert torch.isfinite(seen).all() and torch.isfinite(out).all()
+
+
 def test_either_way_gives_the_same_logits(P):
     """small keys and large queries, the same call planned for short sequences (16-row workgroups) and for long ones"""
     s = setup_written(P, [150, 100], 140, k_by=2.0 ** -24, q_by=2.0 ** 24, H=2, H_kv=2)
