@@ -385,7 +385,7 @@ PASA_API int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cach
  *   n_max   host: what len is expected not to exceed, 0 for max_pages * page.  The work is divided for this length; longer
  *           sequences are computed as well, only more slowly.
  *   ws      pasa_cache_attn_workspace_bytes(shape, cache, n_max) bytes (host-only helper; 0 on invalid arguments), 256-byte aligned.
- *           It belongs to the call alone: calls that overlap in time need one each.
+ *           What it says for one n_max is enough for every smaller one as well (0 is the largest), though a smaller one may ask for more.  It belongs to the call alone: calls that overlap in time need one each.
  */
 PASA_API size_t pasa_cache_attn_workspace_bytes(const pasa_shape_t* shape, const pasa_cache_t* cache, int32_t n_max);
 PASA_API int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t* cache, const void* pool, size_t pool_bytes,

@@ -784,13 +784,20 @@ bool cache_rows_fit(const pasa_shape_t* s, const pasa_cache_t* c) {
   return rows <= ((int64_t)1 << 30) && s->B * ((rows + 255) / 256) < ((int64_t)1 << 31) - 1024;
 }
 
-// How the rows and tokens of a call are divided among workgroups, and the workspace that takes
+// How the rows and tokens of a call are divided among workgroups, and the workspace that takes.  room: bytes there are.  A smaller n_max can ask for more splits, and so
+// for more room, than a larger one (a larger one has longer splits, or is for 256 rows, whose room does not grow): there are then as many as fit, so that
+// a workspace for the longest sequences serves for all.
 struct CacheAttnPlan {
   int wg_rows, splits, pieces, row_tiles, key_parts;
   size_t part_ml, merge, key_range, total;
 };
-CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int32_t n_max) {
+CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int32_t n_max, size_t room = SIZE_MAX) {
   CacheAttnPlan a{};
+  auto lay_out = [&](size_t parts) -> size_t {  // of partial rows and what follows them; -> where that ends
+    a.part_ml = align_up(parts * s->d * 4);
+    a.merge = align_up(a.part_ml + parts * 2 * 4);
+    return a.merge + a.pieces * sizeof(CacheMerge) + 1;  // never zero: that means "invalid"
+  };
   const int64_t capacity = (int64_t)c->max_pages * c->page, tokens = n_max > 0 && n_max < capacity ? n_max : capacity;
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
   // 4, 8 or 16 rows a workgroup (cache_rows_kernel) take time with the runs of 16 rows and the tiles of 64 tokens: 0.0024 us each with groups of 32 of
@@ -806,7 +813,7 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   const bool few = weight * head_tiles * ((rows + 15) / 16) <= 49152 + 14 * head_tiles * a.row_tiles;
   a.wg_rows = rows <= 4 ? 4 : rows <= 8 ? 8 : few ? 16 : 256;
   a.splits = 1;
-  size_t parts = 0;
+  size_t end;
   if (a.wg_rows <= 16) {
     const int64_t wgs = (int64_t)s->B * c->H_kv * ((rows + a.wg_rows - 1) / a.wg_rows);
     // The time of a workgroup is its steps (its four waves take a tile each) and some three more before and after them.  The workgroups of one sequence
@@ -817,24 +824,20 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
     const int resident = 256 * (s->d == 64 ? (c->group == 32 && a.wg_rows == 16 ? 3 : 4) : c->group == 32 || (c->group == 64 && a.wg_rows == 16) ? 2 : 3);
     const int64_t tiles = (tokens + 63) / 64;
     int64_t best = INT64_MAX;
-    for (int n = 1; n <= kCacheMaxSplits && (n == 1 || tokens >= n * 512); ++n) {
+    const size_t rows_all = (size_t)s->B * s->H * s->n;
+    for (int n = 1; n <= kCacheMaxSplits && (n == 1 || (tokens >= n * 512 && align_up(lay_out(rows_all * n)) <= room)); ++n) {
       const int64_t rounds = (wgs * n + resident - 1) / resident, steps = ((tiles + n - 1) / n + 3) / 4;
       const int64_t cost = s->B == 1 ? rounds * (steps + 3) * 64 : wgs * n * (steps + 3) * 64 / resident + (steps + 3) * 32;
       if (cost + (n > 1 ? 128 : 0) < best) { best = cost + (n > 1 ? 128 : 0); a.splits = n; }
     }
-    if (a.splits > 1) parts = (size_t)s->B * s->H * s->n * a.splits;
+    end = lay_out(a.splits > 1 ? rows_all * a.splits : 0);
   } else {
     // one for every compute unit, and if there are fewer than four heads' runs of rows, 64 for each: one head of 40,000 tokens, 128 rows 59 us with 64,
     // 64 with 32, 69 with 128
     a.pieces = (int)std::min<int64_t>(256, 64 * (int64_t)s->B * c->H_kv * a.row_tiles);
-    parts = (size_t)2 * a.pieces * a.wg_rows;
+    end = lay_out((size_t)2 * a.pieces * a.wg_rows);
     // K's magnitudes: runs of a thousand tokens, one pass of a workgroup's threads, unless that are more than the chip takes at once
     a.key_parts = (int)std::max<int64_t>(1, std::min<int64_t>({kCacheMaxKeyParts, 1024 / ((int64_t)s->B * c->H_kv), (tokens + 1023) / 1024}));
-  }
-  a.part_ml = align_up(parts * s->d * 4);
-  a.merge = align_up(a.part_ml + parts * 2 * 4);
-  size_t end = a.merge + a.pieces * sizeof(CacheMerge) + 1;  // never zero: that means "invalid"
-  if (a.wg_rows == 256) {
     // They have the place of the last workgroup's second part, which there never is: what that workgroup starts it also finishes.  More than that holds
     // go behind everything else.
     const size_t slot = (size_t)a.wg_rows * s->d * 4, range = (size_t)s->B * c->H_kv * a.key_parts * 4;
@@ -886,7 +889,7 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   if (!cache_rows_fit(shape, cache)) return PASA_EUNSUPPORTED;
   if (!q || !out || !ws || out == q) return PASA_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned4(lse)) return PASA_EALIGN;
-  const CacheAttnPlan plan = cache_attn_plan(shape, cache, n_max);
+  const CacheAttnPlan plan = cache_attn_plan(shape, cache, n_max, ws_bytes);
   if (ws_bytes < plan.total) return PASA_EWORKSPACE;
   p.q = static_cast<const uint16_t*>(q); p.o = static_cast<uint16_t*>(out); p.lse = lse;
   p.stride_b = shape->stride_b; p.stride_h = shape->stride_h; p.stride_n = shape->stride_n;
