@@ -380,7 +380,8 @@ PASA_API int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cach
  * A row that sees a token of which a group reads back as NaN is NaN, lse included, if it is a group of K, and NaN in the channels of that
  * group, perhaps in others, if it is one of V.  Logits are held in binary32: beyond +-2^30 their spacing makes the weights overflow.  They are
  * good to what binary32 leaves of sum |q| |k|, whatever the magnitudes of q and of the groups of K are, and where calls of many rows are concerned to 2^-26
- * of the largest product |q| |k| that the row makes with any group of the sequence's keys.
+ * of the largest product |q| |k| that the row makes with any group of the sequence's keys.  Queries beyond +-2^100 and sequences whose values sum to more than
+ * 2^120 may overflow; a scale that is infinite in units of log2 (scale * log2(e)) is refused.
  *   q, out  bf16 [B, H, n, d] (shape strides);  lse fp32 [B*H, n] or NULL
  *   n_max   host: what len is expected not to exceed, 0 for max_pages * page.  The work is divided for this length; longer
  *           sequences are computed as well, only more slowly.

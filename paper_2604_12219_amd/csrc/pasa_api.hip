@@ -875,7 +875,7 @@ int pasa_cache_read(const pasa_shape_t* shape, const pasa_cache_t* cache, const 
 
 size_t pasa_cache_attn_workspace_bytes(const pasa_shape_t* shape, const pasa_cache_t* cache, int32_t n_max) {
   if (check_shape(shape, false) != PASA_OK || check_cache(cache) != PASA_OK || n_max < 0) return 0;
-  if (shape->d != cache->d || shape->H % cache->H_kv || !cache_rows_fit(shape, cache)) return 0;
+  if (shape->d != cache->d || shape->H % cache->H_kv || isinf(effective_scale(shape) * 1.4426950408889634f) || !cache_rows_fit(shape, cache)) return 0;
   return cache_attn_plan(shape, cache, n_max).total;
 }
 
@@ -886,6 +886,8 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   const int rc = cache_params(shape, cache, pool, pool_bytes, pages, len, n_new, &p.c);
   if (rc != PASA_OK) return rc;
   if (shape->H % cache->H_kv || n_max < 0) return PASA_EINVAL;
+  p.scale = effective_scale(shape) * 1.4426950408889634f;
+  if (isinf(p.scale)) return PASA_EINVAL;
   if (!cache_rows_fit(shape, cache)) return PASA_EUNSUPPORTED;
   if (!q || !out || !ws || out == q) return PASA_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(ws) || !aligned4(lse)) return PASA_EALIGN;
@@ -894,7 +896,6 @@ int pasa_cache_attn(const void* q, const pasa_shape_t* shape, const pasa_cache_t
   p.q = static_cast<const uint16_t*>(q); p.o = static_cast<uint16_t*>(out); p.lse = lse;
   p.stride_b = shape->stride_b; p.stride_h = shape->stride_h; p.stride_n = shape->stride_n;
   p.H = shape->H; p.share = shape->H / cache->H_kv; p.n = shape->n; p.causal = causal != 0;
-  p.scale = effective_scale(shape) * 1.4426950408889634f;
   p.wg_rows = plan.wg_rows; p.splits = plan.splits;
   p.part_o = static_cast<float*>(ws);
   p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + plan.part_ml);

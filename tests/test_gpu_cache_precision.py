@@ -197,6 +197,21 @@ def test_rows_ahead_of_the_first_token_with_a_small_scale(P):
     assert torch.isfinite(seen).all() and torch.isfinite(out).all()
 
 
+@pytest.mark.parametrize("n", ROWS)
+@pytest.mark.parametrize("v", [-126, -118, -110, -60, 60, 95])
+def test_values_at_every_magnitude(P, n, v):
+    """values of 2^v (and a group of zeros); the smallest are bf16 numbers of few bits, whose scale is 0 in the cache"""
+    kw = dict(H=2, H_kv=1, page=64)
+    s = Setup(P, [200, 3], [200, 3], n=200, **kw)
+    s.v = (s.v.double() * 2.0 ** v).float().bfloat16()
+    s.v[..., 32:64] = 0.0
+    written(s)
+    t = setup(P, [200, 3], n, **kw)
+    t.pool, t.q = s.pool, torch.nn.functional.pad(s.q[:, :, :n], (0, 0, 0, max(0, t.q.shape[2] - 200)))
+    t.pages[:, :s.pages.shape[1]] = s.pages
+    check(t)
+
+
 def test_either_way_gives_the_same_logits(P):
     """small keys and large queries, the same call planned for short sequences (16-row workgroups) and for long ones"""
     s = setup_written(P, [150, 100], 140, k_by=2.0 ** -24, q_by=2.0 ** 24, H=2, H_kv=2)
