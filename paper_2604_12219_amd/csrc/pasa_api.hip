@@ -802,12 +802,12 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
   const int64_t rows = (int64_t)(s->H / c->H_kv) * s->n;
   // 4, 8 or 16 rows a workgroup (cache_rows_kernel) take time with the runs of 16 rows and the tiles of 64 tokens: 0.0024 us each with groups of 32 of
   // 128 channels, 0.002 with groups of 64, 0.0013 with one of 128, 0.0012 with 64 channels.  256 rows (cache_tile_kernel) take time with the tiles, 0.009 us,
-  // 0.0055 with 64 channels, and some 25 us more before and after them.  us, 16 rows / 256:
-  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 17 / 27, 500 rows 18 / 32; 1 head, 200,000 tokens, 33 rows 54 / 107; 40,000, 128 rows 29 / 51; 8
-  //     heads of 20,000, 100 rows 52 / 65; 64 heads of 4000, 33 rows 47 / 70, 64 52 / 71, 128 81 / 78, 192 127 / 84; 40 heads of 75,600, 40 rows 345 / 429,
-  //     64 467 / 437
-  //   groups of 64: 64 heads of 4000, 33 rows 37 / 71; of 128: 64 rows 38 / 68, 128 54 / 75
-  //   d = 64: 64 heads of 4000, 33 rows 25 / 44, 64 32 / 46, 128 45 / 49, 200 77 / 52; 40 heads of 75,600, 64 rows 217 / 270
+  // 0.0055 with 64 channels, and some 30 us more before and after them.  us, 16 rows / 256:
+  //   d = 128, groups of 32: 8 heads, 600 tokens, 128 rows 16 / 32, 500 rows 17 / 38; 1 head, 200,000 tokens, 33 rows 56 / 118; 40,000, 128 rows 29 / 57; 8
+  //     heads of 20,000, 100 rows 52 / 72; 64 heads of 4000, 33 rows 48 / 77, 64 52 / 78, 128 83 / 85, 192 130 / 92; 40 heads of 75,600, 40 rows 347 / 451,
+  //     64 474 / 453
+  //   groups of 64: 64 heads of 4000, 33 rows 38 / 81; of 128: 64 rows 38 / 75, 128 55 / 82
+  //   d = 64: 64 heads of 4000, 33 rows 25 / 49, 64 33 / 51, 128 46 / 55, 200 77 / 57; 40 heads of 75,600, 64 rows 220 / 284
   const double head_tiles = (double)s->B * c->H_kv * ((tokens + 63) / 64), weight = c->group == 128 ? 2 : s->d == 128 && c->group == 32 ? 4 : 3;
   a.row_tiles = (int)((rows + 255) / 256);
   const bool few = weight * head_tiles * ((rows + 15) / 16) <= 49152 + 14 * head_tiles * a.row_tiles;
@@ -832,8 +832,8 @@ CacheAttnPlan cache_attn_plan(const pasa_shape_t* s, const pasa_cache_t* c, int3
     }
     end = lay_out(a.splits > 1 ? rows_all * a.splits : 0);
   } else {
-    // one for every compute unit, and if there are fewer than four heads' runs of rows, 64 for each: one head of 40,000 tokens, 128 rows 59 us with 64,
-    // 64 with 32, 69 with 128
+    // one for every compute unit, and if there are fewer than four heads' runs of rows, 64 for each: one head of 40,000 tokens, 128 rows 58 us with 64,
+    // 62 with 32, 72 with 128
     a.pieces = (int)std::min<int64_t>(256, 64 * (int64_t)s->B * c->H_kv * a.row_tiles);
     end = lay_out((size_t)2 * a.pieces * a.wg_rows);
     // K's magnitudes: runs of a thousand tokens, one pass of a workgroup's threads, unless that are more than the chip takes at once

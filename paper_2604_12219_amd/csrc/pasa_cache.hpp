@@ -38,7 +38,6 @@ struct CacheLayout {
   static constexpr int NG = D / G;         // groups
   static constexpr int CODE = D / 2;       // bytes of a token's codes
   static constexpr int PARAM = 4 * NG;     // bytes of a token's parameters
-  static constexpr int TOKEN = 2 * (CODE + PARAM);
   PASA_DEVICE static uint32_t k_codes(uint32_t) { return 0u; }
   PASA_DEVICE static uint32_t v_codes(uint32_t page) { return page * CODE; }
   PASA_DEVICE static uint32_t k_params(uint32_t page) { return page * (2 * CODE); }

@@ -4,8 +4,9 @@
 // What differs is how a tile gets there: a thread holds a few code words of one token, of K and of V, converts them and writes them
 // to the other half of the ring while this tile is worked on.  The conversion is shared by all rows of a workgroup, hence eight waves
 // and 256 rows: with four waves and 128 it costs twice as much a row.
-// Measured: 3600 rows of 40 heads over 75,600 tokens, d = 128, groups of 32, 5.93 ms, 940 TFLOP/s; 4680 rows of 12 heads over 32,760, 1.00 ms.  Per wave and tile 34
-// matrix and 251 vector instructions (150 in attention over bf16), the matrix cores busy 0.58 and the vector units 0.60 of the cycles at the 1.78 GHz that
+// Measured (median of 23 passes in a row, this kernel alone): 3600 rows of 40 heads over 75,600 tokens, d = 128, groups of 32, 5.99 ms, 930 TFLOP/s; 4680 rows
+// of 12 heads over 32,760, 1.03 ms.  Per wave and tile 34
+// matrix and 252 vector instructions (150 in attention over bf16), the matrix cores busy 0.56 and the vector units 0.59 of the cycles at the 1.79 GHz that
 // the power leaves (bf16: 0.70 at 1.6).  A conversion that costs nothing would take 10 % off, keys rounded to bf16 3 %.
 //
 //   V: bf16(s c + m).  An and-or (and one shift for half of a word) makes fp16 numbers 1024 + c or 64 + c of two codes, a mixed fma
