@@ -19,7 +19,7 @@
 //     2^11.  A cache holds scales down to 2^-126.  So the groups of a key/value head are shifted to the top of fp16's range, each by the power 2^f that
 //     its largest operand over the sequence's tokens allows (cache_key_range_kernel; 2^13 to 2^14 then), and the queries by 2^-f; a row's queries
 //     then by one more power that puts the largest of them between 2^7 and 2^8 (the sum of 128 is an fp16 number), which the row's logit scale takes
-//     back.  So K is exact down to 2^-30 of a group's largest scale and q down to 2^-24 of the row's largest; what is smaller is rounded to 2^-25, that is
+//     back.  So K is exact for scales down to 2^-30 of its group's largest operand and q down to 2^-24 of the row's largest; what is smaller is rounded to 2^-25, that is
 //     2^-38 and 2^-32 of the largest.
 #include "pasa_cache.hpp"
 #include "pasa_cache_pipes.hpp"
